@@ -137,7 +137,7 @@ def prepare(case, seed):
             s["pre"] = normal(M, N, t=torch.bfloat16) if case["act"] != "none" else None
             s["dy"] = normal(M, N, t=torch.bfloat16)
             s["dx"] = torch.zeros(M, K, dtype=torch.bfloat16, device=dev)
-            s["dw"] = torch.zeros(N, K, device=dev)
+            s["dw"] = torch.zeros(N, K, dtype=torch.bfloat16, device=dev)
             s["dbias"] = torch.zeros(N, device=dev)
         if own:
             import paper_2012_09849_b200 as hts
@@ -363,21 +363,40 @@ def _delta(s):
     return _softplus(v) if s["case"]["softplus"] else v
 
 
+def _recurrence(a, b):
+    """h[t] = a[t] h[t-1] + b[t] from h[-1] = 0, for all t at once: maps of 1, 2, 4, ... steps are composed.  a and b are used up."""
+    T, k = a.shape[0], 1
+    a2, b2 = torch.empty_like(a), torch.empty_like(b)
+    while k < T:
+        torch.addcmul(b[k:], a[k:], b[:-k], out=b2[k:])
+        torch.mul(a[k:], a[:-k], out=a2[k:])
+        b2[:k], a2[:k] = b[:k], a[:k]
+        a, a2, b, b2, k = a2, a, b2, b, 2 * k
+    return b
+
+
+def _decays_and_inputs(s, delta, x, b):
+    """[T, N, D, S]: what a step keeps of the state, and what it adds; a step behind its sequence's end keeps all and adds nothing."""
+    a = torch.exp(delta[..., None] * s["a"])
+    a.masked_fill_((s["starts"] != 0)[..., None, None], 0.0)
+    u = (delta * x)[..., None] * b[..., None, :]
+    if s["lengths"] is not None:
+        over = ~_live(s, *x.shape[:2])[..., None, None]
+        a.masked_fill_(over, 1.0)
+        u.masked_fill_(over, 0.0)
+    return a, u
+
+
 def _plain_scan(s):
     c = s["case"]
-    T, N = c["T"], c["N"]
     delta, x, b, cc = _delta(s), s["x"].float(), s["b"].float(), s["c"].float()
-    live, start = _live(s, T, N), s["starts"] != 0
-    h = s["state_in"]
-    y = torch.zeros_like(x)
-    for t in range(T):
-        n = torch.where(start[t][:, None, None], 0.0, h) * torch.exp(delta[t][..., None] * s["a"]) + (delta[t] * x[t])[..., None] * b[t][:, None, :]
-        h = n if s["lengths"] is None else torch.where(live[t][:, None, None], n, h)
-        y[t] = (h * cc[t][:, None, :]).sum(-1)
-    y = y + s["d"] * x
+    a, u = _decays_and_inputs(s, delta, x, b)
+    u[0] += a[0] * s["state_in"]
+    h = _recurrence(a, u)
+    y = (h * cc[..., None, :]).sum(-1) + s["d"] * x
     if s["z"] is not None:
         y = y * _act(s["z"].float(), "silu")
-    return {"y": torch.where(live[..., None], y, 0.0).to(s["x"].dtype), "state_out": h.clone()}
+    return {"y": torch.where(_live(s, c["T"], c["N"])[..., None], y, 0.0).to(s["x"].dtype), "state_out": h[-1].clone()}
 
 
 def _plain_scan_step(s):
@@ -395,48 +414,39 @@ def _plain_scan_step(s):
 
 def _plain_scan_gradient(s):
     c = s["case"]
-    T, N, D, S = c["T"], c["N"], c["D"], c["S"]
     delta, x, b, cc, dy = _delta(s), s["x"].float(), s["b"].float(), s["c"].float(), s["dy"].float()
-    live, start = _live(s, T, N), s["starts"] != 0
-    before = torch.empty(T, N, D, S, device="cuda")             # the state that step t meets
-    h = s["state_in"]
-    for t in range(T):
-        before[t] = torch.where(start[t][:, None, None], 0.0, h)
-        n = before[t] * torch.exp(delta[t][..., None] * s["a"]) + (delta[t] * x[t])[..., None] * b[t][:, None, :]
-        h = n if s["lengths"] is None else torch.where(live[t][:, None, None], n, h)
+    live = _live(s, c["T"], c["N"])
     z = None if s["z"] is None else s["z"].float()
     g = torch.where(live[..., None], dy if z is None else dy * _act(z, "silu"), 0.0)
-    da = torch.zeros(D, S, device="cuda")
-    ddelta, dx, y, db, dc = (torch.zeros(T, N, k, device="cuda") for k in (D, D, D, S, S))
-    carry = s["dstate_out"]
-    for t in reversed(range(T)):
-        kept = before[t] * torch.exp(delta[t][..., None] * s["a"])
-        h = kept + (delta[t] * x[t])[..., None] * b[t][:, None, :]
-        grad = carry + g[t][..., None] * cc[t][:, None, :]
-        if s["lengths"] is not None:
-            grad = torch.where(live[t][:, None, None], grad, 0.0)
-        y[t] = (h * cc[t][:, None, :]).sum(-1)
-        dc[t] = (h * g[t][..., None]).sum(1)
-        db[t] = (grad * (delta[t] * x[t])[..., None]).sum(1)
-        gb = (grad * b[t][:, None, :]).sum(-1)
-        dx[t] = delta[t] * gb
-        ddelta[t] = x[t] * gb + (grad * kept * s["a"]).sum(-1)
-        da += (grad * kept * delta[t][..., None]).sum(0)
-        back = torch.where(start[t][:, None, None], 0.0, grad * torch.exp(delta[t][..., None] * s["a"]))
-        carry = back if s["lengths"] is None else torch.where(live[t][:, None, None], back, carry)
-    t_ = s["x"].dtype
-    dx = dx + s["d"] * g
-    draw_ = ddelta
+    a, u = _decays_and_inputs(s, delta, x, b)
+    u[0] += a[0] * s["state_in"]
+    h = _recurrence(a.clone(), u)
+    kept = a * torch.cat([s["state_in"][None], h[:-1]])         # what a step kept of the state before it
+    y = (h * cc[..., None, :]).sum(-1)
+    dc = (h * g[..., None]).sum(2)
+    del h, u
+    # the gradient of the states runs back: what reaches step t from step t + 1 has that step's decay
+    u = g[..., None] * cc[..., None, :]
+    u[-1] += s["dstate_out"]
+    grad = _recurrence(torch.cat([a[1:], torch.zeros_like(a[:1])]).flip(0), u.flip(0)).flip(0)
+    state_in = a[0] * grad[0]
+    grad.masked_fill_(~live[..., None, None], 0.0)
+    db = (grad * (delta * x)[..., None]).sum(2)
+    gb = (grad * b[..., None, :]).sum(-1)
+    grad *= kept
+    ddt = x * gb + (grad * s["a"]).sum(-1)
+    da = (grad * delta[..., None]).sum((0, 1))
+    dx = delta * gb + s["d"] * g
     if c["softplus"]:
-        v = s["dt"].float() if s["dt_bias"] is None else s["dt"].float() + s["dt_bias"]
-        draw_ = ddelta * torch.sigmoid(v)
-    out = {"x": dx.to(t_), "dt": draw_.to(t_), "b": db.to(t_), "c": dc.to(t_)}
+        ddt = ddt * torch.sigmoid(s["dt"].float() if s["dt_bias"] is None else s["dt"].float() + s["dt_bias"])
+    t = s["x"].dtype
+    out = {"x": dx.to(t), "dt": ddt.to(t), "b": db.to(t), "c": dc.to(t)}
     if z is not None:
-        out["z"] = torch.where(live[..., None], dy * (y + s["d"] * x) * _slope(z, "silu"), 0.0).to(t_)
+        out["z"] = torch.where(live[..., None], dy * (y + s["d"] * x) * _slope(z, "silu"), 0.0).to(t)
     out["a"], out["d"] = da, (g * x).sum((0, 1))
     if s["dt_bias"] is not None:
-        out["dt_bias"] = draw_.sum((0, 1))
-    out["state_in"] = carry.clone()
+        out["dt_bias"] = ddt.sum((0, 1))
+    out["state_in"] = state_in
     return out
 
 
@@ -454,7 +464,7 @@ def _plain_linear_gradient(s):
     dz = s["dy"].float()
     if s["pre"] is not None:
         dz = dz * _slope(s["pre"].float(), s["case"]["act"])
-    return {"dx": (dz @ s["w"].float()).to(torch.bfloat16), "dw": dz.t() @ s["x"].float(), "dbias": dz.sum(0)}
+    return {"dx": (dz @ s["w"].float()).to(torch.bfloat16), "dw": (dz.t() @ s["x"].float()).to(torch.bfloat16), "dbias": dz.sum(0)}
 
 
 _own = {"conv": _own_conv, "conv-step": _own_conv_step, "conv-gradient": _own_conv_gradient, "scan": _own_scan, "scan-step": _own_scan_step,
@@ -471,7 +481,7 @@ def work(case):
         if kind == "linear":
             kept = case["keep"] + case["residual"]
             return {"bytes": 2 * (M * K + N * K + M * N * (1 + kept)) + 4 * N * case["bias"], "flops": 2 * M * N * K}
-        return {"bytes": 2 * (2 * M * K + N * K + M * N * (1 + (case["act"] != "none"))) + 4 * (N * K + N), "flops": 4 * M * N * K}
+        return {"bytes": 2 * (2 * M * K + 2 * N * K + M * N * (1 + (case["act"] != "none"))) + 4 * N, "flops": 4 * M * N * K}
     e = 4 if case["type"] == "fp32" else 2
     D, step = case["D"], kind.endswith("step")
     R = case["N"] if step else _steps(case)
