@@ -369,6 +369,117 @@ hts_status hts_policy_step_noalloc(const hts_net_desc *desc, const hts_weights *
                                    float *values, float *entropy, float *logits_or_null,
                                    void *cuda_stream);
 
+/* ---- the recurrent core of a policy with memory -------------------------------------
+ * A policy that sees only part of the state carries a state of its own from step to step
+ * (the paper's football scenarios are such).  Its core is the chain
+ *   linear -> causal convolution -> linear (dt, B, C) -> selective scan, gated -> linear + residual
+ * over the [T,N] storage for the learner (and prompts of T tokens), with the gradients of each,
+ * and one step at a time for the actor, whose states lie in a pool by slot.
+ *
+ * Rows.  Step t of sequence n is row r = t*N + n.  A tensor of rows has `channels` (or `state`)
+ * adjacent elements per row and starts row r at r * ld elements: a column range of a wider tensor
+ * will do.  Element types are given by dtype (fp32 or bf16); weights, states, sums and
+ * the gradients of weights and states are fp32.
+ *   starts   DEVICE u8 [T,N] or NULL: non-zero = step t is the first of an episode: nothing before it
+ *            is seen.  With a [T+1,N] array whose rows 1..T are the dones that hts_gae reads, row 0 those of
+ *            the rollout before, `starts` is that array and `dones` the same one row further on.
+ *   lengths  DEVICE i32 [N] or NULL: sequence n has lengths[n] steps (held to 0..T), the rows behind
+ *            them are neither read nor written; NULL = all have T.
+ *   slots    DEVICE i32 [N] or NULL: row n's entry of a pool of `pool` states or windows; NULL = entry n.  A row
+ *            whose slot lies outside [0, pool) is skipped (a batch padded to a captured
+ *            size): nothing of it is written.  No slot may occur twice.
+ * Workspaces are the caller's: DEVICE memory on a 16-byte boundary, at least as many bytes as the
+ * function of the same name and `_workspace` returns (0 for sizes that the call refuses), not used by anything else
+ * until the call's work is done; its contents need not be kept.  Calls with workspaces of their own
+ * are independent, also across streams, threads and captured graphs.  Nothing is allocated.       */
+#define HTS_ACT_NONE 0
+#define HTS_ACT_RELU 1
+#define HTS_ACT_SILU 2 /* v / (1 + exp(-v))          */
+#define HTS_ACT_GELU 3 /* v (1 + erf(v / sqrt 2)) / 2 */
+
+typedef struct {
+    int32_t T, N, channels;
+    int32_t width;              /* taps, 2..4                                       */
+    int32_t dtype;              /* of x, y, the windows, dy and dx                  */
+    int32_t activation;         /* HTS_ACT_NONE or HTS_ACT_SILU                     */
+    int64_t ld_x, ld_y;
+    int64_t ld_dy, ld_dx;       /* read by hts_causal_conv_gradient only            */
+} hts_conv_desc;
+
+/* Every channel convolved over the last `width` steps of its sequence:
+ *   y[t,n,c] = act(bias[c] + sum_k w[c,k] x[t-width+1+k, n, c])
+ * where a step before the first is taken from window_in, and one that an episode start lies behind is 0.
+ *   w DEVICE f32 [channels,width];  bias_or_null DEVICE f32 [channels]
+ *   window_in_or_null, window_out_or_null  DEVICE [N,width-1,channels]: the inputs before step 0 (NULL = zeros), oldest
+ *            first, and those that a step behind the last would see (zero where an episode started since)
+ * Errors: INVALID_ARG, CUDA.                                                            */
+hts_status hts_causal_conv(const hts_conv_desc *desc, const void *x, const float *w, const float *bias_or_null,
+                           const uint8_t *starts_or_null, const int32_t *lengths_or_null, const void *window_in_or_null,
+                           void *y, void *window_out_or_null, void *cuda_stream);
+
+/* One step of each of N rows (desc->T is not read): x, y rows [N], starts [N], windows [pool,width-1,channels].
+ * window_out may be window_in.  Outputs equal those of hts_causal_conv bit for bit.          */
+hts_status hts_causal_conv_step(const hts_conv_desc *desc, const void *x, const float *w, const float *bias_or_null,
+                                const uint8_t *starts_or_null, const int32_t *slots_or_null, int32_t pool,
+                                const void *window_in, void *y, void *window_out, void *cuda_stream);
+
+/* The gradients, given dy and (or NULL for zeros) that of window_out, dwindow_out DEVICE f32 [N,width-1,channels].
+ *   dx rows (not those behind a sequence's end);  dw f32 [channels,width];  dbias f32 [channels];
+ *   dwindow_in f32 [N,width-1,channels]: each may be NULL, not all.  Overwritten.
+ * The workspace is needed for dw and dbias only; sums in a fixed order.                        */
+int64_t hts_causal_conv_workspace(int32_t T, int32_t N, int32_t channels, int32_t width);
+hts_status hts_causal_conv_gradient(const hts_conv_desc *desc, const void *x, const float *w, const float *bias_or_null,
+                                    const uint8_t *starts_or_null, const int32_t *lengths_or_null,
+                                    const void *window_in_or_null, const void *dy, const float *dwindow_out_or_null,
+                                    void *dx, float *dw, float *dbias, float *dwindow_in, void *workspace,
+                                    int64_t workspace_bytes, void *cuda_stream);
+
+typedef struct {
+    int32_t T, N, channels;
+    int32_t state;              /* states per channel, 1..64                        */
+    int32_t dtype;              /* of x, dt, b, c, z, y and their gradients         */
+    int32_t softplus;           /* non-zero: delta = log(1 + exp(dt + dt_bias)), else delta = dt + dt_bias */
+    int64_t ld_x, ld_dt, ld_b, ld_c, ld_z, ld_y;
+} hts_scan_desc;
+
+typedef struct {
+    const void *x, *dt;         /* rows of `channels`                               */
+    const void *b, *c;          /* rows of `state`                                  */
+    const void *z;              /* rows of `channels` or NULL: the gate             */
+    const float *a;             /* DEVICE f32 [channels,state]                      */
+    const float *d, *dt_bias;   /* DEVICE f32 [channels], each or NULL              */
+    const uint8_t *starts;      /* or NULL                                          */
+    const int32_t *lengths;     /* or NULL                                          */
+    const float *state_in;      /* DEVICE f32 [N,channels,state] or NULL: zeros     */
+} hts_scan_inputs;
+
+/* The selective scan: for every channel c and state s of sequence n,
+ *   h_s <- (start ? 0 : h_s) exp(delta a[c,s]) + delta x B_s
+ *   y    = (sum_s C_s h_s + d[c] x) silu(z)                  (without the factor if z is NULL)
+ * with delta, x, z of the channel and B, C of the step: hts_gae's recurrence, forwards, with a decay that the data decide.
+ *   y rows of `channels`;  state_out_or_null DEVICE f32 [N,channels,state]: the states after the last steps
+ * Errors: INVALID_ARG, CUDA.                                                            */
+int64_t hts_selective_scan_workspace(int32_t T, int32_t N, int32_t channels, int32_t state, int32_t gradient);
+hts_status hts_selective_scan(const hts_scan_desc *desc, const hts_scan_inputs *in, void *y, float *state_out_or_null,
+                              void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/* One step of each of N rows (desc->T is not read, in->lengths must be NULL): rows [N], starts [N], in->state_in and
+ * state_out [pool,channels,state]; state_out may be state_in.                                */
+hts_status hts_selective_scan_step(const hts_scan_desc *desc, const hts_scan_inputs *in, const int32_t *slots_or_null,
+                                   int32_t pool, void *y, float *state_out, void *cuda_stream);
+
+/* The gradients, given that of y (rows, ld_dy) and that of state_out (or NULL for zeros).  Each may be NULL, not
+ * all; rows behind a sequence's end are not written; sums in a fixed order.            */
+typedef struct {
+    void *x, *dt, *b, *c, *z;   /* rows, dtype                                      */
+    float *a, *d, *dt_bias;     /* as the inputs                                    */
+    float *state_in;            /* [N,channels,state]                               */
+    int64_t ld_x, ld_dt, ld_b, ld_c, ld_z;
+} hts_scan_grads;
+hts_status hts_selective_scan_gradient(const hts_scan_desc *desc, const hts_scan_inputs *in, const void *dy, int64_t ld_dy,
+                                       const float *dstate_out_or_null, const hts_scan_grads *grads, void *workspace,
+                                       int64_t workspace_bytes, void *cuda_stream);
+
 /* Number of kernel launches this library has enqueued since it was loaded
  * (all contexts, all streams); for launch accounting by a benchmark.              */
 uint64_t hts_launch_count(void);

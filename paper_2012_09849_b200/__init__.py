@@ -28,7 +28,9 @@ EXPORTS = ("hts_policy_create", "hts_policy_load_weights", "hts_policy_step", "h
            "hts_policy_evaluate", "hts_policy_gradient", "hts_a2c_terms", "hts_ppo_terms", "hts_delayed_update",
            "hts_policy_read_activation", "hts_action_uniforms", "hts_policy_profile", "hts_policy_profile_read",
            "hts_policy_kernel_name", "hts_last_async_error", "hts_policy_destroy", "hts_gae",
-           "hts_gae_host", "hts_gae_host_release", "hts_vtrace", "hts_policy_step_noalloc", "hts_wait_selftest", "hts_launch_count", "hts_last_cuda_error", "hts_status_string")
+           "hts_gae_host", "hts_gae_host_release", "hts_vtrace", "hts_causal_conv", "hts_causal_conv_step", "hts_causal_conv_gradient",
+           "hts_causal_conv_workspace", "hts_selective_scan", "hts_selective_scan_step", "hts_selective_scan_gradient",
+           "hts_selective_scan_workspace", "hts_policy_step_noalloc", "hts_wait_selftest", "hts_launch_count", "hts_last_cuda_error", "hts_status_string")
 
 
 class HtsError(RuntimeError):
@@ -50,6 +52,25 @@ class hts_weights(C.Structure):
 
 class hts_grads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in WEIGHT_NAMES]
+
+
+class hts_conv_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "N", "channels", "width", "dtype", "activation")] + \
+               [(n, C.c_int64) for n in ("ld_x", "ld_y", "ld_dy", "ld_dx")]
+
+
+class hts_scan_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "N", "channels", "state", "dtype", "softplus")] + \
+               [(n, C.c_int64) for n in ("ld_x", "ld_dt", "ld_b", "ld_c", "ld_z", "ld_y")]
+
+
+class hts_scan_inputs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "dt", "b", "c", "z", "a", "d", "dt_bias", "starts", "lengths", "state_in")]
+
+
+class hts_scan_grads(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "dt", "b", "c", "z", "a", "d", "dt_bias", "state_in")] + \
+               [(n, C.c_int64) for n in ("ld_x", "ld_dt", "ld_b", "ld_c", "ld_z")]
 
 
 _lib = None
@@ -108,6 +129,20 @@ def lib():
         L.hts_gae_host_release.restype = C.c_int
         L.hts_policy_step_noalloc.argtypes = [C.POINTER(hts_net_desc), C.POINTER(hts_weights)] + step[1:]
         L.hts_policy_step_noalloc.restype = C.c_int
+        conv, scan = C.POINTER(hts_conv_desc), [C.POINTER(hts_scan_desc), C.POINTER(hts_scan_inputs)]
+        L.hts_causal_conv.argtypes = [conv] + [vp] * 9
+        L.hts_causal_conv_step.argtypes = [conv] + [vp] * 5 + [i32] + [vp] * 4
+        L.hts_causal_conv_gradient.argtypes = [conv] + [vp] * 13 + [C.c_int64, vp]
+        L.hts_selective_scan.argtypes = scan + [vp, vp, vp, C.c_int64, vp]
+        L.hts_selective_scan_step.argtypes = scan + [vp, i32, vp, vp, vp]
+        L.hts_selective_scan_gradient.argtypes = scan + [vp, C.c_int64, vp, C.POINTER(hts_scan_grads), vp, C.c_int64, vp]
+        for name in ("hts_causal_conv", "hts_selective_scan"):
+            for form in ("", "_step", "_gradient"):
+                getattr(L, name + form).restype = C.c_int
+        L.hts_causal_conv_workspace.argtypes = [i32] * 4
+        L.hts_causal_conv_workspace.restype = C.c_int64
+        L.hts_selective_scan_workspace.argtypes = [i32] * 5
+        L.hts_selective_scan_workspace.restype = C.c_int64
         L.hts_launch_count.restype = C.c_uint64
         L.hts_last_cuda_error.restype = C.c_char_p
         L.hts_status_string.restype = C.c_char_p
@@ -259,6 +294,53 @@ def hts_gae_host(rewards, values, dones, bootstrap, gamma, lam, T, N, advantages
 def hts_vtrace(log_rhos, rewards, values, dones, bootstrap, gamma, lam, rho_bar, c_bar, T, N, vs, pg_advantages,
                stream=None) -> None:
     _native.vtrace(log_rhos, rewards, values, dones, bootstrap, gamma, lam, rho_bar, c_bar, T, N, vs, pg_advantages, stream)
+
+
+# ---- the recurrent core: sizes, element types and row strides are read off the tensors ------
+# Rows are [T, N, channels] tensors ([N, channels] in the steps) of the current device: evenly spaced, their elements adjacent (a
+# column range of a wider tensor will do).  Optional arguments are None.
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+def hts_causal_conv(x, w, bias, starts, lengths, window_in, activation, y, window_out, stream=None) -> None:
+    """activation: "none" or "silu"."""
+    _native.causal_conv(x, w, bias, starts, lengths, window_in, ACTIVATIONS[activation], y, window_out, stream)
+
+
+def hts_causal_conv_step(x, w, bias, starts, slots, window_in, activation, y, window_out, stream=None) -> None:
+    """window_in, window_out: [pool, width - 1, channels]; they may be one tensor."""
+    _native.causal_conv_step(x, w, bias, starts, slots, window_in, ACTIVATIONS[activation], y, window_out, stream)
+
+
+def hts_causal_conv_gradient(x, w, bias, starts, lengths, window_in, activation, dy, dwindow_out, dx, dw, dbias, dwindow_in, workspace,
+                             stream=None) -> None:
+    _native.causal_conv_gradient(x, w, bias, starts, lengths, window_in, ACTIVATIONS[activation], dy, dwindow_out, dx, dw, dbias, dwindow_in, workspace,
+                                 stream)
+
+
+def hts_causal_conv_workspace(T, N, channels, width) -> int:
+    """Bytes of the workspace of hts_causal_conv_gradient."""
+    return lib().hts_causal_conv_workspace(int(T), int(N), int(channels), int(width))
+
+
+def hts_selective_scan(x, dt, a, b, c, d, dt_bias, z, starts, lengths, state_in, softplus, y, state_out, workspace, stream=None) -> None:
+    _native.selective_scan(x, dt, a, b, c, d, dt_bias, z, starts, lengths, state_in, softplus, y, state_out, workspace, stream)
+
+
+def hts_selective_scan_step(x, dt, a, b, c, d, dt_bias, z, starts, slots, state_in, softplus, y, state_out, stream=None) -> None:
+    """state_in, state_out: [pool, channels, state]; they may be one tensor."""
+    _native.selective_scan_step(x, dt, a, b, c, d, dt_bias, z, starts, slots, state_in, softplus, y, state_out, stream)
+
+
+def hts_selective_scan_gradient(x, dt, a, b, c, d, dt_bias, z, starts, lengths, state_in, softplus, dy, dstate_out, grads: dict, workspace,
+                                stream=None) -> None:
+    """grads: tensors to write under the names x, dt, a, b, c, d, dt_bias, z, state_in, shaped like the inputs; what is not asked for is left out."""
+    _native.selective_scan_gradient(x, dt, a, b, c, d, dt_bias, z, starts, lengths, state_in, softplus, dy, dstate_out, grads, workspace, stream)
+
+
+def hts_selective_scan_workspace(T, N, channels, state, gradient=False) -> int:
+    """Bytes of the workspace of hts_selective_scan, or of its gradient."""
+    return lib().hts_selective_scan_workspace(int(T), int(N), int(channels), int(state), int(bool(gradient)))
 
 
 def hts_gae_host_release() -> None:

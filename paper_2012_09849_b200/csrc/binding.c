@@ -121,6 +121,141 @@ static int to_stream(PyObject *x, void **out)
     return !PyErr_Occurred();
 }
 
+/* ---- tensors of the recurrent core: the library is told sizes and strides, so that they are read off the tensors ---- */
+static PyObject *g_types[4], *s_dtype, *s_shape, *s_stride, *s_get_device, *s_nbytes;      /* torch.float32, bfloat16, uint8, int32 */
+static PyTypeObject *g_tensor;
+enum { F32_T = 0, BF16_T = 1, U8_T = 2, I32_T = 3 };                                 /* the first two are HTS_DTYPE_* */
+
+static int torch_types(void)
+{
+    static const char *const names[4] = {"float32", "bfloat16", "uint8", "int32"};
+    if (g_tensor) return 1;
+    PyObject *torch = PyImport_ImportModule("torch"), *c = torch ? PyObject_GetAttrString(torch, "_C") : NULL;
+    for (int i = 0; c && i < 4; ++i)
+        if (!g_types[i] && !(g_types[i] = PyObject_GetAttrString(torch, names[i]))) Py_CLEAR(c);
+    if (c && !g_get_device) g_get_device = PyObject_GetAttrString(c, "_cuda_getDevice");
+    PyObject *t = c && g_get_device ? PyObject_GetAttrString(torch, "Tensor") : NULL;
+    Py_XDECREF(torch); Py_XDECREF(c);
+    g_tensor = (PyTypeObject *)t;
+    return t != NULL;
+}
+static int refuse(PyObject *type, const char *name, const char *why)
+{
+    PyErr_Format(type, "%s %s", name, why);
+    return 0;
+}
+static int int64_at(PyObject *tuple, Py_ssize_t i, int64_t *out)
+{
+    *out = PyLong_AsLongLong(PyTuple_GET_ITEM(tuple, i));
+    return !(*out == -1 && PyErr_Occurred());
+}
+/* A tensor: its type, sizes and strides (at most four).  want < 0: of fp32 or bf16. */
+typedef struct { int type, dims; int64_t size[4], stride[4]; void *ptr; } Seen;
+static int look(PyObject *x, const char *name, int want, Seen *v)
+{
+    if (!torch_types()) return 0;
+    if (!PyObject_TypeCheck(x, g_tensor)) return refuse(PyExc_TypeError, name, "is not a tensor");
+    PyObject *t = PyObject_GetAttr(x, s_dtype);
+    if (!t) return 0;
+    for (v->type = 0; v->type < 4 && t != g_types[v->type]; ++v->type) { }
+    Py_DECREF(t);
+    if (want < 0 ? v->type > BF16_T : v->type != want) return refuse(PyExc_TypeError, name, "has the wrong element type");
+    PyObject *sz = PyObject_GetAttr(x, s_shape), *st = sz ? PyObject_CallMethodNoArgs(x, s_stride) : NULL;
+    int ok = st && PyTuple_Check(sz) && PyTuple_Check(st) && PyTuple_GET_SIZE(sz) <= 4;
+    v->dims = ok ? (int)PyTuple_GET_SIZE(sz) : 0;
+    for (int i = 0; ok && i < v->dims; ++i) ok = int64_at(sz, i, &v->size[i]) && int64_at(st, i, &v->stride[i]);
+    Py_XDECREF(sz); Py_XDECREF(st);
+    if (!ok) return PyErr_Occurred() ? 0 : refuse(PyExc_ValueError, name, "has the wrong shape");
+    return int_ptr(PyObject_CallMethodNoArgs(x, s_data_ptr), &v->ptr);
+}
+/* memory of the current CUDA device */
+static int here(PyObject *x, const char *name)
+{
+    PyObject *at = PyObject_CallMethodNoArgs(x, s_get_device);
+    const long d = at ? PyLong_AsLong(at) : -1;
+    Py_XDECREF(at);
+    if (!at || (d == -1 && PyErr_Occurred())) return 0;
+    if (d < 0) return refuse(PyExc_ValueError, name, "is not on a CUDA device");
+    PyObject *cur = PyObject_CallNoArgs(g_get_device);
+    const long c = cur ? PyLong_AsLong(cur) : -1;
+    Py_XDECREF(cur);
+    if (!cur || (c == -1 && PyErr_Occurred())) return 0;
+    return c == d || refuse(PyExc_ValueError, name, "is not on the current device");
+}
+/* Rows: [d0, cols], or [d0, d1, cols] with d1 > 0, the rows evenly spaced and their elements adjacent.  None is NULL. */
+static int to_rows(PyObject *x, const char *name, int64_t d0, int64_t d1, int64_t cols, int type, void **ptr, int64_t *ld)
+{
+    *ptr = NULL; *ld = 0;
+    if (x == Py_None) return 1;
+    Seen v;
+    const int lead = d1 > 0 ? 2 : 1;
+    if (!look(x, name, type, &v)) return 0;
+    if (v.dims != lead + 1 || v.size[0] != d0 || (lead == 2 && v.size[1] != d1) || v.size[lead] != cols) return refuse(PyExc_ValueError, name, "has the wrong shape");
+    int ok = cols == 1 || v.stride[lead] == 1;
+    if (lead == 2 && d1 > 1) { *ld = v.stride[1]; ok = ok && (d0 == 1 || v.stride[0] == d1 * *ld); }
+    else *ld = d0 > 1 ? v.stride[0] : cols;
+    if (!ok || *ld < cols) return refuse(PyExc_ValueError, name, "needs evenly spaced rows of adjacent elements");
+    *ptr = v.ptr;
+    return here(x, name);
+}
+/* A dense tensor of the given sizes (0 ends them).  None is NULL. */
+static int to_dense(PyObject *x, const char *name, int type, int64_t a, int64_t b, int64_t c, void **ptr)
+{
+    *ptr = NULL;
+    if (x == Py_None) return 1;
+    Seen v;
+    const int64_t want[3] = {a, b, c};
+    const int dims = c ? 3 : b ? 2 : 1;
+    if (!look(x, name, type, &v)) return 0;
+    int ok = v.dims == dims;
+    for (int i = 0; ok && i < dims; ++i) ok = v.size[i] == want[i];
+    if (!ok) return refuse(PyExc_ValueError, name, "has the wrong shape");
+    int64_t dense = 1;
+    for (int i = dims - 1; i >= 0; --i) {
+        if (v.size[i] > 1 && v.stride[i] != dense) return refuse(PyExc_ValueError, name, "must be contiguous");
+        dense *= v.size[i];
+    }
+    *ptr = v.ptr;
+    return here(x, name);
+}
+/* Device memory of any type: its address and bytes.  None is NULL. */
+static int to_workspace(PyObject *x, void **ptr, int64_t *bytes)
+{
+    *ptr = NULL; *bytes = 0;
+    if (x == Py_None) return 1;
+    if (!torch_types()) return 0;
+    if (!PyObject_TypeCheck(x, g_tensor)) return refuse(PyExc_TypeError, "workspace", "is not a tensor");
+    PyObject *n = PyObject_GetAttr(x, s_nbytes);
+    *bytes = n ? PyLong_AsLongLong(n) : -1;
+    Py_XDECREF(n);
+    return *bytes >= 0 && to_ptr(x, ptr) && here(x, "workspace");
+}
+/* [N, width], or [T, N, width]: the tensor that the others follow */
+static int to_lead(PyObject *x, const char *name, int lead, int32_t *dtype, int64_t *T, int64_t *N, int64_t *width)
+{
+    Seen v;
+    if (!look(x, name, -1, &v)) return 0;
+    if (v.dims != lead + 1) return refuse(PyExc_ValueError, name, "has the wrong shape");
+    for (int i = 0; i < v.dims; ++i)
+        if (v.size[i] < 1 || v.size[i] > INT32_MAX) return refuse(PyExc_ValueError, name, "has the wrong shape");
+    *dtype = v.type; *T = lead == 2 ? v.size[0] : 0; *N = v.size[lead - 1]; *width = v.size[lead];
+    return 1;
+}
+/* the size of a tensor's dimension i, of `dims` */
+static int to_size(PyObject *x, const char *name, int type, int dims, int i, int64_t *out)
+{
+    Seen v;
+    if (!look(x, name, type, &v)) return 0;
+    if (v.dims != dims || v.size[i] < 1 || v.size[i] > INT32_MAX) return refuse(PyExc_ValueError, name, "has the wrong shape");
+    *out = v.size[i];
+    return 1;
+}
+static PyObject *entry(PyObject *dict, const char *key)                 /* borrowed; None if there is no such key */
+{
+    PyObject *v = PyDict_GetItemString(dict, key);
+    return v ? v : Py_None;
+}
+
 static int weights_of(PyObject *map, void **p)
 {
     for (int i = 0; i < 12; ++i) {
@@ -239,6 +374,114 @@ FN(vtrace)
     PTR(vs, 11); PTR(pg, 12); STREAM(13);
     CALL(hts_vtrace(lr, r, v, d, b, gamma, lambda, rho, c, T, N, vs, pg, stream), "hts_vtrace");
 }
+#define ROWS(x, name, d0, d1, cols, ptr, ld) if (!to_rows(x, name, d0, d1, cols, dtype, (void **)&(ptr), &(ld))) return NULL
+#define DENSE(x, name, type, d0, d1, d2, ptr) if (!to_dense(x, name, type, d0, d1, d2, (void **)&(ptr))) return NULL
+
+static PyObject *conv_like(PyObject *const *a, Py_ssize_t nargs, int form)        /* 0: all steps, 1: one step, 2: gradient */
+{
+    ARGS(form == 2 ? 15 : 10);
+    const int lead = form == 1 ? 1 : 2;
+    int32_t dtype;
+    int64_t T, N, D, W, pool = 0, bytes = 0;
+    hts_conv_desc d = {0};
+    void *x, *y = NULL, *dy = NULL, *dx = NULL, *win, *wout = NULL, *work = NULL;
+    float *w, *bias, *dwout = NULL, *dw = NULL, *db = NULL, *dwin = NULL;
+    uint8_t *starts;
+    int32_t *index;
+    if (!to_lead(a[0], "x", lead, &dtype, &T, &N, &D) || !to_size(a[1], "w", F32_T, 2, 1, &W)) return NULL;
+    if (W < 2 || W > 4) { refuse(PyExc_ValueError, "w", "needs two to four taps"); return NULL; }
+    const int64_t d0 = lead == 2 ? T : N, d1 = lead == 2 ? N : 0;
+    ROWS(a[0], "x", d0, d1, D, x, d.ld_x);
+    DENSE(a[1], "w", F32_T, D, W, 0, w);
+    DENSE(a[2], "bias", F32_T, D, 0, 0, bias);
+    DENSE(a[3], "starts", U8_T, d0, d1, 0, starts);
+    DENSE(a[4], form == 1 ? "slots" : "lengths", I32_T, N, 0, 0, index);
+    if (form == 1 && !to_size(a[5], "window_in", dtype, 3, 0, &pool)) return NULL;
+    DENSE(a[5], "window_in", dtype, form == 1 ? pool : N, W - 1, D, win);
+    I32(act, 6);
+    d.T = (int32_t)T; d.N = (int32_t)N; d.channels = (int32_t)D; d.width = (int32_t)W; d.dtype = dtype; d.activation = act;
+    if (form == 2) {
+        ROWS(a[7], "dy", T, N, D, dy, d.ld_dy);
+        DENSE(a[8], "dwindow_out", F32_T, N, W - 1, D, dwout);
+        ROWS(a[9], "dx", T, N, D, dx, d.ld_dx);
+        DENSE(a[10], "dw", F32_T, D, W, 0, dw);
+        DENSE(a[11], "dbias", F32_T, D, 0, 0, db);
+        DENSE(a[12], "dwindow_in", F32_T, N, W - 1, D, dwin);
+        if (!to_workspace(a[13], &work, &bytes)) return NULL;
+        STREAM(14);
+        CALL(hts_causal_conv_gradient(&d, x, w, bias, starts, index, win, dy, dwout, dx, dw, db, dwin, work, bytes, stream), "hts_causal_conv_gradient");
+    }
+    ROWS(a[7], "y", d0, d1, D, y, d.ld_y);
+    DENSE(a[8], "window_out", dtype, form == 1 ? pool : N, W - 1, D, wout);
+    STREAM(9);
+    if (form == 1) { CALL(hts_causal_conv_step(&d, x, w, bias, starts, index, (int32_t)pool, win, y, wout, stream), "hts_causal_conv_step"); }
+    CALL(hts_causal_conv(&d, x, w, bias, starts, index, win, y, wout, stream), "hts_causal_conv");
+}
+FN(causal_conv) { (void)self; return conv_like(a, nargs, 0); }
+FN(causal_conv_step) { (void)self; return conv_like(a, nargs, 1); }
+FN(causal_conv_gradient) { (void)self; return conv_like(a, nargs, 2); }
+
+static PyObject *scan_like(PyObject *const *a, Py_ssize_t nargs, int form)
+{
+    ARGS(form == 2 ? 17 : form == 1 ? 15 : 16);
+    const int lead = form == 1 ? 1 : 2;
+    int32_t dtype;
+    int64_t T, N, D, S, pool = 0, bytes = 0, ld_dy = 0;
+    hts_scan_desc d = {0};
+    hts_scan_inputs in = {0};
+    hts_scan_grads g = {0};
+    void *y = NULL, *dy = NULL, *work = NULL;
+    float *sout = NULL, *dsout = NULL;
+    int32_t *index;
+    if (!to_lead(a[0], "x", lead, &dtype, &T, &N, &D) || !to_size(a[2], "a", F32_T, 2, 1, &S)) return NULL;
+    const int64_t d0 = lead == 2 ? T : N, d1 = lead == 2 ? N : 0;
+    ROWS(a[0], "x", d0, d1, D, in.x, d.ld_x);
+    ROWS(a[1], "dt", d0, d1, D, in.dt, d.ld_dt);
+    DENSE(a[2], "a", F32_T, D, S, 0, in.a);
+    ROWS(a[3], "b", d0, d1, S, in.b, d.ld_b);
+    ROWS(a[4], "c", d0, d1, S, in.c, d.ld_c);
+    DENSE(a[5], "d", F32_T, D, 0, 0, in.d);
+    DENSE(a[6], "dt_bias", F32_T, D, 0, 0, in.dt_bias);
+    ROWS(a[7], "z", d0, d1, D, in.z, d.ld_z);
+    DENSE(a[8], "starts", U8_T, d0, d1, 0, in.starts);
+    DENSE(a[9], form == 1 ? "slots" : "lengths", I32_T, N, 0, 0, index);
+    if (form == 1 && !to_size(a[10], "state_in", F32_T, 3, 0, &pool)) return NULL;
+    DENSE(a[10], "state_in", F32_T, form == 1 ? pool : N, D, S, in.state_in);
+    const int soft = PyObject_IsTrue(a[11]);
+    if (soft < 0) return NULL;
+    d.T = (int32_t)T; d.N = (int32_t)N; d.channels = (int32_t)D; d.state = (int32_t)S; d.dtype = dtype; d.softplus = soft;
+    if (form != 1) in.lengths = index;
+    if (form == 2) {
+        ROWS(a[12], "dy", d0, d1, D, dy, ld_dy);
+        DENSE(a[13], "dstate_out", F32_T, N, D, S, dsout);
+        if (!PyDict_Check(a[14])) { PyErr_SetString(PyExc_TypeError, "grads is not a dict"); return NULL; }
+        ROWS(entry(a[14], "x"), "grads['x']", d0, d1, D, g.x, g.ld_x);
+        ROWS(entry(a[14], "dt"), "grads['dt']", d0, d1, D, g.dt, g.ld_dt);
+        ROWS(entry(a[14], "b"), "grads['b']", d0, d1, S, g.b, g.ld_b);
+        ROWS(entry(a[14], "c"), "grads['c']", d0, d1, S, g.c, g.ld_c);
+        ROWS(entry(a[14], "z"), "grads['z']", d0, d1, D, g.z, g.ld_z);
+        DENSE(entry(a[14], "a"), "grads['a']", F32_T, D, S, 0, g.a);
+        DENSE(entry(a[14], "d"), "grads['d']", F32_T, D, 0, 0, g.d);
+        DENSE(entry(a[14], "dt_bias"), "grads['dt_bias']", F32_T, D, 0, 0, g.dt_bias);
+        DENSE(entry(a[14], "state_in"), "grads['state_in']", F32_T, N, D, S, g.state_in);
+        if (!to_workspace(a[15], &work, &bytes)) return NULL;
+        STREAM(16);
+        CALL(hts_selective_scan_gradient(&d, &in, dy, ld_dy, dsout, &g, work, bytes, stream), "hts_selective_scan_gradient");
+    }
+    ROWS(a[12], "y", d0, d1, D, y, d.ld_y);
+    DENSE(a[13], "state_out", F32_T, form == 1 ? pool : N, D, S, sout);
+    if (form == 1) {
+        STREAM(14);
+        CALL(hts_selective_scan_step(&d, &in, index, (int32_t)pool, y, sout, stream), "hts_selective_scan_step");
+    }
+    if (!to_workspace(a[14], &work, &bytes)) return NULL;
+    STREAM(15);
+    CALL(hts_selective_scan(&d, &in, y, sout, work, bytes, stream), "hts_selective_scan");
+}
+FN(selective_scan) { (void)self; return scan_like(a, nargs, 0); }
+FN(selective_scan_step) { (void)self; return scan_like(a, nargs, 1); }
+FN(selective_scan_gradient) { (void)self; return scan_like(a, nargs, 2); }
+
 static PyObject *init(PyObject *self, PyObject *error)
 {
     (void)self;
@@ -249,7 +492,8 @@ static PyObject *init(PyObject *self, PyObject *error)
 #define M(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef kMethods[] = {
     M(policy_step), M(policy_step_host), M(policy_step_indexed), M(policy_evaluate), M(policy_gradient), M(policy_load_weights),
-    M(a2c_terms), M(ppo_terms), M(delayed_update), M(gae), M(gae_host), M(vtrace), {"init", init, METH_O, NULL}, {NULL, NULL, 0, NULL}};
+    M(a2c_terms), M(ppo_terms), M(delayed_update), M(gae), M(gae_host), M(vtrace), M(causal_conv), M(causal_conv_step), M(causal_conv_gradient),
+    M(selective_scan), M(selective_scan_step), M(selective_scan_gradient), {"init", init, METH_O, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", NULL, -1, kMethods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__native(void)
@@ -258,6 +502,11 @@ PyMODINIT_FUNC PyInit__native(void)
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     s_value = PyUnicode_InternFromString("value");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    s_nbytes = PyUnicode_InternFromString("nbytes");
     for (int i = 0; i < 12; ++i) s_weights[i] = PyUnicode_InternFromString(kWeights[i]);
     PyObject *np = PyImport_ImportModule("numpy"), *ct = np ? PyImport_ImportModule("ctypes") : NULL;
     g_ndarray = np ? (PyTypeObject *)PyObject_GetAttrString(np, "ndarray") : NULL;

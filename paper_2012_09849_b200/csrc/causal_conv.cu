@@ -1,0 +1,462 @@
+// Short causal convolution of every channel over the steps of its sequence, with resets at episode starts.
+//
+//   pre[t] = bias + sum_k w[k] v_k,  v_k = x[t - W + 1 + k], from the window before the first step, zero if an episode starts in between
+//   dx[u] = sum over t = u .. u + W - 1 of w[u - t + W - 1] dpre[t], up to the next start;  dw[k] = sum dpre[t] v_k
+//
+// All of it is bound by memory: a step of a channel is read once (the gradient: x and dy) and written once, with 2 W
+// multiply-adds in between.  A thread holds a vector of channels of one sequence and walks a run of steps with the last W - 1
+// inputs in registers, so that no input is read twice inside a run; a run reads the W - 1 before it again.  Neighbouring lanes
+// hold neighbouring channels: every access of a warp is one contiguous piece of a row.
+#include "recurrent.cuh"
+
+namespace hts {
+namespace {
+
+constexpr int kVector = 4;                      // channels of a thread where alignment allows, else one
+constexpr int kWarps = 8, kGroup = 8;           // warps of a block (a run each); steps loaded at once
+
+struct ConvArgs {
+    int T, N, D, lanes, runs, length;           // lanes: vectors of channels; runs per sequence, of `length` steps
+    int64_t ld_x, ld_y, ld_dy, ld_dx;
+    const float *w, *bias;
+    const uint8_t* starts;
+    const int32_t* lengths;
+    bool silu;
+};
+
+// Where a thread works: a vector of channels and a run of steps of one sequence.
+struct Place {
+    int c, n, t0, t1, end;                      // steps [t0, t1) of a sequence with `end` steps
+    bool on, first, last;                       // last: the run that ends the sequence
+};
+template <int V>
+__device__ __forceinline__ Place place(const ConvArgs& p)
+{
+    const int across = (p.lanes + 31) / 32;
+    const int lane = (int)(blockIdx.x % across) * 32 + threadIdx.x;
+    const int64_t unit = (int64_t)(blockIdx.x / across) * kWarps + threadIdx.y;
+    Place q;
+    q.on = lane < p.lanes && unit < (int64_t)p.N * p.runs;
+    const int run = q.on ? (int)(unit / p.N) : 0;
+    q.n = q.on ? (int)(unit % p.N) : 0;
+    q.c = (q.on ? lane : 0) * V;
+    q.end = p.lengths && q.on ? min(max(p.lengths[q.n], 0), p.T) : p.T;
+    q.t0 = min(run * p.length, q.end);
+    q.t1 = min(q.t0 + p.length, q.end);
+    q.first = run == 0;
+    q.last = q.on && q.t1 == q.end && (q.t0 < q.end || q.first);
+    return q;
+}
+
+template <int V, int W>
+__device__ __forceinline__ void push(float (&win)[W][V], const float (&v)[V])
+{
+#pragma unroll
+    for (int k = 0; k + 1 < W; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
+#pragma unroll
+    for (int i = 0; i < V; ++i) win[W - 1][i] = v[i];
+}
+template <int V, int W>
+__device__ __forceinline__ void clear(float (&win)[W][V])
+{
+#pragma unroll
+    for (int k = 0; k < W; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) win[k][i] = 0.f;
+}
+// The W inputs before step t0 (the oldest is not used again): the window, or the steps before the run.
+template <typename T, int V, int W>
+__device__ __forceinline__ void enter(const ConvArgs& p, const Place& q, const T* x, const T* window, float (&win)[W][V])
+{
+    clear(win);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+        float v[V] = {};
+        if (q.first) {
+            if (window) {
+                const Vec<T, V> r = load_vec<V>(window + ((size_t)q.n * (W - 1) + j) * p.D + q.c);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = to_float(r.v[i]);
+            }
+        } else {                                // runs are at least W - 1 steps long
+            const size_t row = (size_t)(q.t0 - (W - 1) + j) * p.N + q.n;
+            if (p.starts && p.starts[row]) clear(win);
+            const Vec<T, V> r = load_vec<V>(x + row * p.ld_x + q.c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = to_float(r.v[i]);
+        }
+        push(win, v);
+    }
+}
+template <int V, int W>
+__device__ __forceinline__ void weights(const ConvArgs& p, int c, float (&w)[W][V], float (&b)[V])
+{
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        b[i] = p.bias ? p.bias[c + i] : 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) w[k][i] = p.w[(size_t)(c + i) * W + k];
+    }
+}
+
+template <typename T, int V, int W>
+__global__ void __launch_bounds__(32 * kWarps) conv_kernel(const ConvArgs p, const T* x, const T* window_in, T* y, T* window_out)
+{
+    pdl_wait();
+    pdl_trigger();
+    const Place q = place<V>(p);
+    if (!q.on) return;
+    float w[W][V], b[V], win[W][V];
+    weights(p, q.c, w, b);
+    if (q.t0 < q.end || q.last) enter<T, V, W>(p, q, x, window_in, win);
+    for (int t = q.t0; t < q.t1; t += kGroup) {
+        Vec<T, V> raw[kGroup];
+        uint8_t st[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            const size_t row = (size_t)min(t + j, q.t1 - 1) * p.N + q.n;
+            raw[j] = load_vec<V>(x + row * p.ld_x + q.c);
+            st[j] = p.starts ? p.starts[row] : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j)
+            if (t + j < q.t1) {
+                float v[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = to_float(raw[j].v[i]);
+                if (st[j]) clear(win);
+                push(win, v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float a = b[i];
+#pragma unroll
+                    for (int k = 0; k < W; ++k) a = fmaf(w[k][i], win[k][i], a);
+                    v[i] = p.silu ? silu(a) : a;
+                }
+                store_vec<V>(y + ((size_t)(t + j) * p.N + q.n) * p.ld_y + q.c, v);
+            }
+    }
+    if (q.last && window_out) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) store_vec<V>(window_out + ((size_t)q.n * (W - 1) + j) * p.D + q.c, win[j + 1]);
+    }
+}
+
+// One step of row n over the window at its slot; a row whose slot lies outside the pool is left alone.
+template <typename T, int V, int W>
+__global__ void __launch_bounds__(128) conv_step_kernel(const ConvArgs p, const T* x, const int32_t* slots, int pool, const T* window_in, T* y, T* window_out)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int64_t id = (int64_t)blockIdx.x * 128 + threadIdx.x;
+    if (id >= (int64_t)p.N * p.lanes) return;
+    const int n = (int)(id / p.lanes), c = (int)(id % p.lanes) * V;
+    const int slot = slots ? slots[n] : n;
+    if (slot < 0 || slot >= pool) return;
+    Vec<T, V> old[W - 1], now = load_vec<V>(x + (size_t)n * p.ld_x + c);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) old[j] = load_vec<V>(window_in + ((size_t)slot * (W - 1) + j) * p.D + c);
+    const bool fresh = p.starts && p.starts[n];
+    float w[W][V], b[V], win[W][V], v[V];
+    weights(p, c, w, b);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) win[j][i] = fresh ? 0.f : to_float(old[j].v[i]);
+        win[W - 1][i] = to_float(now.v[i]);
+        float a = b[i];
+#pragma unroll
+        for (int k = 0; k < W; ++k) a = fmaf(w[k][i], win[k][i], a);
+        v[i] = p.silu ? silu(a) : a;
+    }
+    store_vec<V>(y + (size_t)n * p.ld_y + c, v);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) store_vec<V>(window_out + ((size_t)slot * (W - 1) + j) * p.D + c, win[j + 1]);
+}
+
+// A run walks W - 1 steps past its end, for the terms that those steps add to its inputs' gradients.  `pend[j]`: the gradient
+// of the input W - 1 - j steps back, complete when it reaches j = 0.  part: [block of runs][W + 1][D], weights then bias.
+template <typename T, int V, int W>
+__global__ void __launch_bounds__(32 * kWarps) conv_gradient_kernel(const ConvArgs p, const T* x, const T* window_in, const T* dy, const float* dwindow_out,
+                                                                    T* dx, float* dwindow_in, float* part)
+{
+    pdl_wait();
+    pdl_trigger();
+    __shared__ float sums[kWarps][(W + 1) * V][33];
+    const Place q = place<V>(p);
+    float dw[W][V] = {}, db[V] = {};
+    if (q.on && (q.t0 < q.end || q.last)) {
+        float w[W][V], b[V], win[W][V], pend[W][V];
+        weights(p, q.c, w, b);
+        enter<T, V, W>(p, q, x, window_in, win);
+        clear(pend);
+        int since = W;                          // steps since the episode's start; W: further back than any tap
+        // the gradient of input u leaves: it is this run's, or the window's and the run is the first
+        auto leave = [&](int u, const float (&g)[V]) {
+            if (u >= q.t0) {
+                if (dx) store_vec<V>(dx + ((size_t)u * p.N + q.n) * p.ld_dx + q.c, g);
+            } else if (q.first && dwindow_in)
+                store_vec<V>(dwindow_in + ((size_t)q.n * (W - 1) + u + W - 1) * p.D + q.c, g);
+        };
+        constexpr int G = 4;
+        const int stop = min(q.t1 + W - 1, q.end);
+        for (int t = q.t0; t < stop; t += G) {
+            Vec<T, V> rx[G], rg[G];
+            uint8_t st[G];
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                const size_t row = (size_t)min(t + j, stop - 1) * p.N + q.n;
+                rx[j] = load_vec<V>(x + row * p.ld_x + q.c);
+                rg[j] = load_vec<V>(dy + row * p.ld_dy + q.c);
+                st[j] = p.starts ? p.starts[row] : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < G; ++j)
+                if (t + j < stop) {
+                    float v[V], g[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[i] = to_float(rx[j].v[i]);
+                    if (st[j]) { clear(win); since = 0; }
+                    else since = min(since + 1, W);
+                    push(win, v);
+                    const bool mine = t + j < q.t1;
+                    const float zero[V] = {};
+                    push(pend, zero);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float a = b[i];
+#pragma unroll
+                        for (int k = 0; k < W; ++k) a = fmaf(w[k][i], win[k][i], a);
+                        g[i] = to_float(rg[j].v[i]);
+                        if (p.silu) g[i] *= silu_slope(a);
+                        if (mine) {
+                            db[i] += g[i];
+#pragma unroll
+                            for (int k = 0; k < W; ++k) dw[k][i] = fmaf(g[i], win[k][i], dw[k][i]);
+                        }
+#pragma unroll
+                        for (int k = 0; k < W; ++k) pend[k][i] = W - 1 - k <= since ? fmaf(w[k][i], g[i], pend[k][i]) : pend[k][i];
+                    }
+                    leave(t + j - (W - 1), pend[0]);
+                }
+        }
+        if (stop == q.end) {                    // the window after the sequence holds its last inputs
+#pragma unroll
+            for (int j = 1; j < W; ++j) {
+                const int u = q.end - W + j;
+                if (u >= q.t1) continue;        // the next run's
+                float g[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    g[i] = pend[j][i];
+                    if (dwindow_out && W - 1 - j <= since) g[i] += dwindow_out[((size_t)q.n * (W - 1) + j - 1) * p.D + q.c + i];
+                }
+                leave(u, g);
+            }
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) sums[threadIdx.y][k * V + i][threadIdx.x] = dw[k][i];
+        sums[threadIdx.y][W * V + i][threadIdx.x] = db[i];
+    }
+    __syncthreads();
+    const int across = (p.lanes + 31) / 32, c0 = (int)(blockIdx.x % across) * 32 * V;
+    for (int e = threadIdx.y * 32 + threadIdx.x; e < (W + 1) * 32 * V; e += 32 * kWarps) {
+        const int k = e / (32 * V), c = e % (32 * V);
+        float a = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) a += sums[i][k * V + c % V][c / V];
+        if (c0 + c < p.D) part[((size_t)(blockIdx.x / across) * (W + 1) + k) * p.D + c0 + c] = a;
+    }
+}
+
+__global__ void __launch_bounds__(1024) column_sums_kernel(const ColumnSums p)
+{
+    pdl_wait();
+    pdl_trigger();
+    __shared__ float s[32][33];
+    const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
+    float a[4] = {};
+    if (c < p.cols) {
+        int64_t r = threadIdx.y;
+        for (; r + 96 < p.rows; r += 128)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[j] += p.part[(r + 32 * j) * p.cols + c];
+        for (; r < p.rows; r += 32) a[0] += p.part[r * p.cols + c];
+    }
+    s[threadIdx.y][threadIdx.x] = (a[0] + a[1]) + (a[2] + a[3]);
+    __syncthreads();
+    float v = s[threadIdx.x][threadIdx.y];              // a warp per column now
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    const int64_t col = (int64_t)blockIdx.x * 32 + threadIdx.y;
+    if (threadIdx.x == 0 && col < p.cols) {
+        if (col < p.split) {
+            if (p.first) p.first[(col % p.inner) * p.outer + col / p.inner] = v;
+        } else if (col < p.split2) {
+            if (p.second) p.second[col - p.split] = v;
+        } else if (p.third)
+            p.third[col - p.split2] = v;
+    }
+}
+
+// Runs of steps: enough threads for two thousand on every SM, `least` steps at least.
+void cut_runs(ConvArgs& p, int V, int least)
+{
+    p.lanes = p.D / V;
+    const int64_t want = ceil_div((int64_t)kCoreSms * 2048, (int64_t)p.N * p.lanes);
+    const int64_t length = ceil_div(ceil_div(p.T, want), kGroup) * kGroup;
+    p.length = (int)(length < least ? least : length);
+    p.runs = (int)ceil_div(p.T, p.length);
+}
+int64_t run_blocks(const ConvArgs& p) { return ceil_div((int64_t)p.N * p.runs, kWarps); }
+// Whether vectors of channels of every tensor start on a boundary of their own size.
+bool vectors(int64_t D, size_t bytes, std::initializer_list<const void*> pointers, std::initializer_list<int64_t> strides)
+{
+    bool ok = D % kVector == 0;
+    for (const void* q : pointers) ok = ok && aligned_to(q, bytes);
+    for (int64_t l : strides) ok = ok && l % kVector == 0;
+    return ok;
+}
+
+constexpr int kGradientRun = 16;
+ConvArgs conv_args(const hts_conv_desc& d, const float* w, const float* bias, const uint8_t* starts, const int32_t* lengths)
+{
+    ConvArgs p{};
+    p.T = d.T; p.N = d.N; p.D = d.channels; p.ld_x = d.ld_x; p.ld_y = d.ld_y; p.ld_dy = d.ld_dy; p.ld_dx = d.ld_dx;
+    p.w = w; p.bias = bias; p.starts = starts; p.lengths = lengths; p.silu = d.activation == HTS_ACT_SILU;
+    return p;
+}
+
+template <typename F>
+hts_status by_width(int width, F f)
+{
+    switch (width) {
+    case 2: return f(std::integral_constant<int, 2>());
+    case 3: return f(std::integral_constant<int, 3>());
+    default: return f(std::integral_constant<int, 4>());
+    }
+}
+
+template <typename T>
+hts_status forward(ConvArgs p, int width, const T* x, const T* win, T* y, T* wout, cudaStream_t s)
+{
+    const bool wide = vectors(p.D, kVector * sizeof(T), {x, win, y, wout}, {p.ld_x, p.ld_y});
+    cut_runs(p, wide ? kVector : 1, kGroup);
+    const int64_t blocks = run_blocks(p) * ceil_div(p.lanes, 32);
+    if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
+    return by_width(width, [&](auto k) {
+        constexpr int W = decltype(k)::value;
+        HTS_CUDA(launch_pdl(wide ? conv_kernel<T, kVector, W> : conv_kernel<T, 1, W>, dim3((unsigned)blocks), dim3(32, kWarps), 0, s, p, x, win, y, wout));
+        note_launch();
+        return HTS_OK;
+    });
+}
+template <typename T>
+hts_status step(ConvArgs p, int width, const T* x, const int32_t* slots, int pool, const T* win, T* y, T* wout, cudaStream_t s)
+{
+    const bool wide = vectors(p.D, kVector * sizeof(T), {x, win, y, wout}, {p.ld_x, p.ld_y});
+    p.lanes = p.D / (wide ? kVector : 1);
+    const int64_t blocks = ceil_div((int64_t)p.N * p.lanes, 128);
+    if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
+    return by_width(width, [&](auto k) {
+        constexpr int W = decltype(k)::value;
+        HTS_CUDA(launch_pdl(wide ? conv_step_kernel<T, kVector, W> : conv_step_kernel<T, 1, W>, dim3((unsigned)blocks), dim3(128), 0, s, p, x, slots, pool, win, y, wout));
+        note_launch();
+        return HTS_OK;
+    });
+}
+template <typename T>
+hts_status gradient(ConvArgs p, int width, const T* x, const T* win, const T* dy, const float* dwout, T* dx, float* dw, float* db, float* dwin, float* part,
+                    cudaStream_t s)
+{
+    const bool wide = vectors(p.D, kVector * sizeof(T), {x, win, dy, dx}, {p.ld_x, p.ld_dy, dx ? p.ld_dx : 0}) && aligned_to(dwin, 16);
+    cut_runs(p, wide ? kVector : 1, kGradientRun);
+    const int64_t rows = run_blocks(p), blocks = rows * ceil_div(p.lanes, 32);
+    if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
+    const bool sums = dw || db;
+    const hts_status st = by_width(width, [&](auto k) {
+        constexpr int W = decltype(k)::value;
+        HTS_CUDA(launch_pdl(wide ? conv_gradient_kernel<T, kVector, W> : conv_gradient_kernel<T, 1, W>, dim3((unsigned)blocks), dim3(32, kWarps), 0, s, p, x, win, dy,
+                            dwout, dx, dwin, sums ? part : nullptr));
+        note_launch();
+        return HTS_OK;
+    });
+    if (st != HTS_OK || !sums) return st;
+    const int64_t cols = (int64_t)(width + 1) * p.D;
+    return launch_column_sums({part, rows, cols, (int64_t)width * p.D, p.D, width, dw, db, cols, nullptr}, s);
+}
+
+bool bad(const hts_conv_desc* d, bool with_steps)
+{
+    return !d || (with_steps && d->T < 1) || d->N < 1 || d->channels < 1 || d->width < 2 || d->width > 4 || d->ld_x < d->channels ||
+           (d->dtype != HTS_DTYPE_FP32 && d->dtype != HTS_DTYPE_BF16) || (d->activation != HTS_ACT_NONE && d->activation != HTS_ACT_SILU);
+}
+
+}  // namespace
+
+hts_status launch_column_sums(const ColumnSums& p, cudaStream_t s)
+{
+    HTS_CUDA(launch_pdl(column_sums_kernel, dim3((unsigned)ceil_div(p.cols, 32)), dim3(32, 32), 0, s, p));
+    note_launch();
+    return HTS_OK;
+}
+
+}  // namespace hts
+
+using namespace hts;
+
+extern "C" int64_t hts_causal_conv_workspace(int32_t T, int32_t N, int32_t channels, int32_t width)
+{
+    if (T < 1 || N < 1 || channels < 1 || width < 2 || width > 4) return 0;
+    int64_t rows = 0;
+    for (int V : {1, kVector}) {                // whichever form the pointers' alignment allows
+        if (channels % V) continue;
+        ConvArgs p{};
+        p.T = T; p.N = N; p.D = channels;
+        cut_runs(p, V, kGradientRun);
+        if (run_blocks(p) > rows) rows = run_blocks(p);
+    }
+    return (int64_t)round256((size_t)rows * (width + 1) * channels * sizeof(float));
+}
+
+extern "C" hts_status hts_causal_conv(const hts_conv_desc* d, const void* x, const float* w, const float* bias, const uint8_t* starts, const int32_t* lengths,
+                                      const void* window_in, void* y, void* window_out, void* stream)
+{
+    if (bad(d, true) || !x || !w || !y || d->ld_y < d->channels || y == x || (window_out && window_out == window_in)) return HTS_ERR_INVALID_ARG;
+    const ConvArgs p = conv_args(*d, w, bias, starts, lengths);
+    if (d->dtype == HTS_DTYPE_FP32)
+        return forward(p, d->width, (const float*)x, (const float*)window_in, (float*)y, (float*)window_out, (cudaStream_t)stream);
+    return forward(p, d->width, (const __nv_bfloat16*)x, (const __nv_bfloat16*)window_in, (__nv_bfloat16*)y, (__nv_bfloat16*)window_out, (cudaStream_t)stream);
+}
+
+extern "C" hts_status hts_causal_conv_step(const hts_conv_desc* d, const void* x, const float* w, const float* bias, const uint8_t* starts, const int32_t* slots,
+                                           int32_t pool, const void* window_in, void* y, void* window_out, void* stream)
+{
+    if (bad(d, false) || !x || !w || !y || !window_in || !window_out || d->ld_y < d->channels || y == x || pool < 1 || (!slots && pool < d->N)) return HTS_ERR_INVALID_ARG;
+    const ConvArgs p = conv_args(*d, w, bias, starts, nullptr);
+    if (d->dtype == HTS_DTYPE_FP32)
+        return step(p, d->width, (const float*)x, slots, pool, (const float*)window_in, (float*)y, (float*)window_out, (cudaStream_t)stream);
+    return step(p, d->width, (const __nv_bfloat16*)x, slots, pool, (const __nv_bfloat16*)window_in, (__nv_bfloat16*)y, (__nv_bfloat16*)window_out, (cudaStream_t)stream);
+}
+
+extern "C" hts_status hts_causal_conv_gradient(const hts_conv_desc* d, const void* x, const float* w, const float* bias, const uint8_t* starts, const int32_t* lengths,
+                                               const void* window_in, const void* dy, const float* dwindow_out, void* dx, float* dw, float* dbias,
+                                               float* dwindow_in, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (bad(d, true) || !x || !w || !dy || d->ld_dy < d->channels || (dx && d->ld_dx < d->channels) || (dx && (dx == x || dx == dy)) || (!dx && !dw && !dbias && !dwindow_in))
+        return HTS_ERR_INVALID_ARG;
+    if ((dw || dbias) && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < hts_causal_conv_workspace(d->T, d->N, d->channels, d->width)))
+        return HTS_ERR_INVALID_ARG;
+    const ConvArgs p = conv_args(*d, w, bias, starts, lengths);
+    float* part = (float*)workspace;
+    if (d->dtype == HTS_DTYPE_FP32)
+        return gradient(p, d->width, (const float*)x, (const float*)window_in, (const float*)dy, dwindow_out, (float*)dx, dw, dbias, dwindow_in, part, (cudaStream_t)stream);
+    return gradient(p, d->width, (const __nv_bfloat16*)x, (const __nv_bfloat16*)window_in, (const __nv_bfloat16*)dy, dwindow_out, (__nv_bfloat16*)dx, dw, dbias, dwindow_in,
+                    part, (cudaStream_t)stream);
+}

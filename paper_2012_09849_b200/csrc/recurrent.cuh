@@ -1,0 +1,56 @@
+// What the kernels of the recurrent core share: rows of [T, N, channels], short vectors of channels, activations, sums over rows.
+#pragma once
+#include "common.cuh"
+
+namespace hts {
+
+// Work is cut by the number of SMs of a B200; a constant, so that a workspace's size does not depend on the device that is asked.
+constexpr int kCoreSms = 148;
+
+inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline size_t round256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+// The sums of the columns of part[rows][cols], in a fixed order: column c of the first `split` goes to
+// first[(c % inner) * outer + c / inner], of those before `split2` to second[c - split], of the others to third[c - split2].
+// A null destination is skipped.
+struct ColumnSums {
+    const float* part;
+    int64_t rows, cols, split, inner, outer;
+    float *first, *second;
+    int64_t split2;
+    float* third;
+};
+hts_status launch_column_sums(const ColumnSums& p, cudaStream_t s);
+
+#ifdef __CUDACC__
+template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16(v); }
+
+template <int V, typename T>
+__device__ __forceinline__ Vec<T, V> load_vec(const T* p) { return *reinterpret_cast<const Vec<T, V>*>(p); }
+template <int V, typename T>
+__device__ __forceinline__ void store_vec(T* p, const float (&f)[V])
+{
+    Vec<T, V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.v[i] = from_float<T>(f[i]);
+    *reinterpret_cast<Vec<T, V>*>(p) = r;
+}
+
+// 1 / (1 + exp(-v)): 0 and 1 at the infinities
+__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+__device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
+__device__ __forceinline__ float silu_slope(float v)
+{
+    const float q = sigmoid(v);
+    return q * (1.f + v * (1.f - q));
+}
+#endif
+
+}  // namespace hts

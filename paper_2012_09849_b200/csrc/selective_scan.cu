@@ -1,0 +1,834 @@
+// Selective state space scan: an affine recurrence per channel and state whose decay and input depend on the data, with resets
+// at episode starts.
+//
+//   delta = softplus(dt + bias),  h_s <- (start ? 0 : h_s) exp(delta A_s) + delta x B_s,  y = (sum_s C_s h_s + D x) silu(z)
+//
+// A channel's S states share delta, x, z and y, the channels of a step share B and C.  A thread holds up to sixteen states of
+// one channel in registers and walks the steps; neighbouring lanes hold neighbouring channels, so that a warp reads and writes
+// contiguous pieces of a row, and B and C go to shared memory once per block and step.  Per state and step that leaves one
+// exponential and four multiply-adds (two per instruction).
+//
+// Where the sequences and channels alone do not fill the device, the steps are cut into runs.  A run is an affine map of the state:
+// decay exp(A_s sum delta), or 0 after a start, and its end from a zero state.  One kernel takes all runs' maps, one composes
+// them in order, and the scan starts every run from its own state.  The gradient's recurrence runs back over the same steps
+// and is cut the same way.
+//
+// States, sums and decays are fp32 whatever the inputs' type; outputs are rounded once.
+#include "recurrent.cuh"
+#include "f32x2.cuh"
+
+namespace hts {
+namespace {
+
+constexpr int kThreads = 128, kGroup = 8;       // threads of a block; steps staged at once
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct ScanArgs {
+    int T, N, D, S;
+    int runs, length;                           // runs per sequence, of `length` steps
+    int64_t ld_x, ld_dt, ld_b, ld_c, ld_z, ld_y;
+    const float *a, *d, *dt_bias;
+    const uint8_t* starts;
+    const int32_t* lengths;
+    bool softplus;
+};
+// The runs' maps: ends [run][N][D][S] (overwritten by the runs' first states), sums of delta [run][N][D], whether a run has a
+// start [run][N].  The gradient's: what a run hands back of its own outputs' gradients [run][N][D][S].
+struct RunMaps {
+    float *ends, *sums, *back;
+    uint8_t* broken;
+};
+
+__device__ __forceinline__ float exp2_approx(float v)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 exp2_pair(f32x2 v) { return pair(exp2_approx(lane_of(v, 0)), exp2_approx(lane_of(v, 1))); }
+
+// log(1 + exp(v)) = max(v, 0) + log(1 + e), e = exp(-|v|); log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by atanh's power
+// series: the first term left out is below 2e-8 of the sum.  `slope`: its derivative.
+__device__ __forceinline__ float softplus(float v, float* slope = nullptr)
+{
+    const float e = __expf(-fabsf(v)), s = __fdividef(e, 2.f + e), q = s * s;
+    float r = 1.f / 13.f;
+    r = fmaf(r, q, 1.f / 11.f);
+    r = fmaf(r, q, 1.f / 9.f);
+    r = fmaf(r, q, 1.f / 7.f);
+    r = fmaf(r, q, 1.f / 5.f);
+    r = fmaf(r, q, 1.f / 3.f);
+    r = fmaf(r, q, 1.f);
+    if (slope) *slope = __fdividef(v >= 0.f ? 1.f : e, 1.f + e);
+    return fmaxf(v, 0.f) + 2.f * s * r;
+}
+__device__ __forceinline__ int steps_of(const int32_t* lengths, int n, int T) { return lengths ? min(max(lengths[n], 0), T) : T; }
+
+// SP states of A, times log2(e), as pairs; zero behind the last state.
+template <int SP>
+__device__ __forceinline__ void load_decays(const ScanArgs& p, int ch, int s0, bool on, f32x2 (&a2)[SP / 2])
+{
+#pragma unroll
+    for (int i = 0; i < SP / 2; ++i) {
+        float v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) v[k] = on && s0 + 2 * i + k < p.S ? p.a[(size_t)ch * p.S + s0 + 2 * i + k] * kLog2e : 0.f;
+        a2[i] = pair(v[0], v[1]);
+    }
+}
+// The states from s0 of a channel, [..][D][S].
+template <int SP>
+__device__ __forceinline__ void load_states(const ScanArgs& p, const float* from, size_t row, int ch, int s0, bool on, f32x2 (&h)[SP / 2])
+{
+#pragma unroll
+    for (int i = 0; i < SP / 2; ++i) {
+        float v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) v[k] = from && on && s0 + 2 * i + k < p.S ? from[(row * p.D + ch) * p.S + s0 + 2 * i + k] : 0.f;
+        h[i] = pair(v[0], v[1]);
+    }
+}
+template <int SP>
+__device__ __forceinline__ void store_states(const ScanArgs& p, float* to, size_t row, int ch, int s0, bool on, const f32x2 (&h)[SP / 2])
+{
+#pragma unroll
+    for (int i = 0; i < SP; ++i)
+        if (on && s0 + i < p.S) to[(row * p.D + ch) * p.S + s0 + i] = lane_of(h[i / 2], i & 1);
+}
+// B and C of steps t .. t + STEPS - 1 of sequence n as fp32, zero behind the last state and at steps from `end` on.
+template <typename T, int STEPS, int SP, int NT>
+__device__ __forceinline__ void stage_bc(const ScanArgs& p, const T* b, const T* c, int n, int t, int end, float (*sb)[SP], float (*sc)[SP])
+{
+#pragma unroll
+    for (int e0 = 0; e0 < STEPS * SP; e0 += NT) {
+        const int e = e0 + threadIdx.x, j = e / SP, s = e % SP;
+        if (STEPS * SP % NT && e >= STEPS * SP) break;
+        const bool on = s < p.S && t + j < end;
+        const size_t row = (size_t)(t + j) * p.N + n;
+        sb[j][s] = on ? to_float(b[row * p.ld_b + s]) : 0.f;
+        sc[j][s] = on && c ? to_float(c[row * p.ld_c + s]) : 0.f;
+    }
+}
+
+enum Mode { SCAN, MAPS, MAPS_BACK };            // outputs; the runs' maps; those and what the runs hand back
+
+// SPT states a thread, LS lanes a channel.  dy: MAPS_BACK only, in the place of y.
+template <typename T, int SPT, int LS, Mode MODE>
+__global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const T* x, const T* dt, const T* b, const T* c, const T* z, const T* dy, const float* first,
+                                                        T* y, float* state_out, RunMaps m)
+{
+    constexpr int SP = SPT * LS, CB = kThreads / LS;
+    __shared__ __align__(16) float sb[2][kGroup][SP], sc[2][kGroup][SP];
+    __shared__ uint8_t fresh[2][kGroup];
+    pdl_wait();
+    pdl_trigger();
+    const int across = (p.D + CB - 1) / CB;
+    const int n = (int)(blockIdx.x / across % p.N), run = (int)(blockIdx.x / across / p.N);
+    const int sub = threadIdx.x % LS, own = (int)(blockIdx.x % across) * CB + threadIdx.x / LS, s0 = sub * SPT;
+    const bool on = own < p.D;
+    const int ch = on ? own : 0;
+    const int end = steps_of(p.lengths, n, p.T);
+    const int t0 = min(run * p.length, end), t1 = min(t0 + p.length, end);
+
+    f32x2 a2[SPT / 2], h[SPT / 2], prod[SPT / 2], back[SPT / 2];
+    load_decays<SPT>(p, ch, s0, on, a2);
+    load_states<SPT>(p, MODE == SCAN ? first : nullptr, (size_t)run * p.N + n, ch, s0, on, h);
+    if (MODE == MAPS_BACK)
+#pragma unroll
+        for (int i = 0; i < SPT / 2; ++i) { prod[i] = both(1.f); back[i] = both(0.f); }
+    const float skip = p.d && on ? p.d[ch] : 0.f, bias = p.dt_bias && on ? p.dt_bias[ch] : 0.f;
+    float sum = 0.f;
+    bool broken = false;
+
+    for (int t = t0, buf = 0; t < t1; t += kGroup, buf ^= 1) {
+        stage_bc<T, kGroup, SP, kThreads>(p, b, MODE == MAPS ? nullptr : c, n, t, t1, sb[buf], sc[buf]);
+        if (threadIdx.x < kGroup) fresh[buf][threadIdx.x] = p.starts && t + (int)threadIdx.x < t1 ? p.starts[(size_t)(t + threadIdx.x) * p.N + n] : 0;
+        T rx[kGroup], rdt[kGroup], rz[kGroup], rg[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            const size_t row = (size_t)min(t + j, t1 - 1) * p.N + n;
+            rx[j] = x[row * p.ld_x + ch];
+            rdt[j] = dt[row * p.ld_dt + ch];
+            if (MODE != MAPS && z) rz[j] = z[row * p.ld_z + ch];
+            if (MODE == MAPS_BACK) rg[j] = dy[row * p.ld_y + ch];
+        }
+        __syncthreads();                        // the other buffer's readers have passed the barrier before
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+            if (t + j >= t1) break;
+            const float xv = to_float(rx[j]), raw = to_float(rdt[j]) + bias, delta = p.softplus ? softplus(raw) : raw;
+            if (fresh[buf][j]) {
+#pragma unroll
+                for (int i = 0; i < SPT / 2; ++i) h[i] = both(0.f);
+                broken = true;
+            }
+            sum += delta;
+            const f32x2 d2 = both(delta), u2 = both(delta * xv);
+            float g = 0.f;
+            if (MODE == MAPS_BACK) {
+                g = to_float(rg[j]);
+                if (z) g *= silu(to_float(rz[j]));
+            }
+            f32x2 acc[2] = {both(0.f), both(0.f)};
+#pragma unroll
+            for (int i = 0; i < SPT / 2; i += 2) {
+                const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[buf][j][s0 + 2 * i]);
+                const f32x2 bb[2] = {bv.x, bv.y};
+                f32x2 cc[2] = {0, 0};
+                if (MODE != MAPS) {
+                    const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[buf][j][s0 + 2 * i]);
+                    cc[0] = cv.x; cc[1] = cv.y;
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const f32x2 decay = exp2_pair(mul2(d2, a2[i + k]));
+                    h[i + k] = fma2(decay, h[i + k], mul2(u2, bb[k]));
+                    if (MODE == SCAN) acc[k] = fma2(cc[k], h[i + k], acc[k]);
+                    if (MODE == MAPS_BACK && !broken) {
+                        prod[i + k] = mul2(prod[i + k], decay);
+                        back[i + k] = fma2(mul2(both(g), cc[k]), prod[i + k], back[i + k]);
+                    }
+                }
+            }
+            if (MODE == SCAN) {
+                float v = (lane_of(acc[0], 0) + lane_of(acc[1], 0)) + (lane_of(acc[0], 1) + lane_of(acc[1], 1));
+#pragma unroll
+                for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                v = fmaf(skip, xv, v);
+                if (z) v *= silu(to_float(rz[j]));
+                if (on && sub == 0) y[((size_t)(t + j) * p.N + n) * p.ld_y + ch] = from_float<T>(v);
+            }
+        }
+    }
+    if (MODE == SCAN) {
+        if (state_out && run == p.runs - 1) store_states<SPT>(p, state_out, n, ch, s0, on, h);
+    } else {
+        const size_t row = (size_t)run * p.N + n;
+        store_states<SPT>(p, m.ends, row, ch, s0, on, h);
+        if (MODE == MAPS_BACK) store_states<SPT>(p, m.back, row, ch, s0, on, back);
+        if (on && sub == 0) m.sums[row * p.D + ch] = sum;
+        if (threadIdx.x == 0) m.broken[row] = broken;       // the same from every block of the row
+    }
+}
+
+// Composes the runs' maps: ends become the runs' first states, `back` what reaches a run from the ones behind it.
+__global__ void __launch_bounds__(256) compose_kernel(const ScanArgs p, const float* state_in, const float* dstate_out, RunMaps m)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int64_t per = (int64_t)p.D * p.S, id = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)p.N * per;
+    if (id >= all) return;
+    const int n = (int)(id / per);
+    const int64_t chan = id / p.S;                          // n * D + channel
+    const float a2 = p.a[id % per] * kLog2e;
+    float* v = blockIdx.y ? m.back : m.ends;
+    float carry = blockIdx.y ? (dstate_out ? dstate_out[id] : 0.f) : (state_in ? state_in[id] : 0.f);
+    constexpr int G = 8;                                    // loads under way at once
+    for (int i0 = 0; i0 < p.runs; i0 += G) {
+        float e[G] = {}, keep[G] = {};
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            const int r = blockIdx.y ? p.runs - 1 - (i0 + k) : i0 + k;
+            if (r >= 0 && r < p.runs - (blockIdx.y ? 0 : 1)) {           // the last run's end is not asked for
+                e[k] = v[(int64_t)r * all + id];
+                keep[k] = m.broken[(int64_t)r * p.N + n] ? -1.f : exp2_approx(a2 * m.sums[(int64_t)r * p.N * p.D + chan]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < G; ++k) {
+            const int r = blockIdx.y ? p.runs - 1 - (i0 + k) : i0 + k;
+            if (r >= 0 && r < p.runs) {
+                v[(int64_t)r * all + id] = carry;
+                carry = keep[k] < 0.f ? e[k] : fmaf(keep[k], carry, e[k]);
+            }
+        }
+    }
+}
+
+// One step of row n over the states at its slot: four states a thread, LS lanes a channel, ROWS rows that share A.  A row whose slot
+// lies outside the pool is left alone.
+template <typename T, int LS, bool QUADS, int ROWS>
+__global__ void __launch_bounds__(128) scan_step_kernel(const ScanArgs p, const T* x, const T* dt, const T* b, const T* c, const T* z, const int32_t* slots, int pool,
+                                                        const float* state_in, T* y, float* state_out)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int64_t id = (int64_t)blockIdx.x * 128 + threadIdx.x;
+    const int sub = (int)(id % LS), s0 = sub * 4;
+    const int64_t cn = id / LS, groups = (p.N + ROWS - 1) / ROWS;
+    const bool on = cn < p.D * groups;
+    const int ch = on ? (int)(cn % p.D) : 0, n0 = on ? (int)(cn / p.D) * ROWS : 0;
+    float a2[4];
+    if (QUADS) {
+        const float4 v = s0 < p.S ? *reinterpret_cast<const float4*>(p.a + (size_t)ch * p.S + s0) : make_float4(0, 0, 0, 0);
+        a2[0] = v.x; a2[1] = v.y; a2[2] = v.z; a2[3] = v.w;
+    } else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a2[i] = s0 + i < p.S ? p.a[(size_t)ch * p.S + s0 + i] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a2[i] *= kLog2e;
+    const float skip = p.d ? p.d[ch] : 0.f, bias = p.dt_bias ? p.dt_bias[ch] : 0.f;
+    float h[ROWS][4];
+    int slot[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int n = n0 + r;
+        slot[r] = on && n < p.N ? (slots ? slots[n] : n) : -1;
+        if (slot[r] >= pool) slot[r] = -1;
+        const size_t at = ((size_t)max(slot[r], 0) * p.D + ch) * p.S + s0;
+        if (QUADS) {
+            const float4 v = slot[r] >= 0 && s0 < p.S ? *reinterpret_cast<const float4*>(state_in + at) : make_float4(0, 0, 0, 0);
+            h[r][0] = v.x; h[r][1] = v.y; h[r][2] = v.z; h[r][3] = v.w;
+        } else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[r][i] = slot[r] >= 0 && s0 + i < p.S ? state_in[at + i] : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int n = min(n0 + r, p.N - 1);
+        const bool fresh = p.starts && p.starts[n];
+        const float xv = to_float(x[(size_t)n * p.ld_x + ch]), raw = to_float(dt[(size_t)n * p.ld_dt + ch]) + bias, delta = p.softplus ? softplus(raw) : raw;
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float bv = s0 + i < p.S ? to_float(b[(size_t)n * p.ld_b + s0 + i]) : 0.f, cv = s0 + i < p.S ? to_float(c[(size_t)n * p.ld_c + s0 + i]) : 0.f;
+            h[r][i] = fmaf(exp2_approx(delta * a2[i]), fresh ? 0.f : h[r][i], delta * xv * bv);
+            v = fmaf(cv, h[r][i], v);
+        }
+#pragma unroll
+        for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        v = fmaf(skip, xv, v);
+        if (z) v *= silu(to_float(z[(size_t)n * p.ld_z + ch]));
+        if (slot[r] < 0) continue;
+        if (sub == 0) y[(size_t)n * p.ld_y + ch] = from_float<T>(v);
+        const size_t at = ((size_t)slot[r] * p.D + ch) * p.S + s0;
+        if (QUADS) {
+            if (s0 < p.S) *reinterpret_cast<float4*>(state_out + at) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
+        } else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (s0 + i < p.S) state_out[at + i] = h[r][i];
+    }
+}
+
+// ---- gradient ------------------------------------------------------------------------------------------------------------
+struct GradArgs {
+    int64_t ld_dy, ld_dx, ld_ddt, ld_dz;
+    float *checks;                              // states at the chunks' first steps, [block][chunk][quarter][thread] of float4
+    float *part_bc;                             // [channel block][row][2 SP]
+    float *part_ch;                             // [run][N][D S + 2 D]: dA, dD, d(dt_bias)
+    const float *first, *incoming;              // [run][N][D][S]: states at the runs' first steps; gradients from behind the runs
+    float *dstate_in;
+    int chunks;                                 // of kChunk steps, per run
+};
+constexpr int kChunk = 8;
+
+// A run's steps in chunks of kChunk.  Forward through the run, the state at every chunk's first step goes to memory; then the
+// chunks are taken from the last to the first: their states are computed again and kept in shared memory, and the gradient
+// of the state walks back over them.  Sums over channels (dB, dC) are taken from shared memory too: a thread takes four
+// states of a step and adds the products of a share of the block's channels, which costs one load and two packed
+// multiply-adds for four terms, where exchanges between lanes would take two of each for every term.
+template <typename T, int SPT, int LS>
+__global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs p, const GradArgs q, const T* x, const T* dt, const T* b, const T* c, const T* z,
+                                                                 const T* dy, T* dx, T* ddt, T* dz)
+{
+    constexpr int SP = SPT * LS, CB = kThreads / LS, Q = SPT / 4, ITEMS = kChunk * CB / kThreads;
+    extern __shared__ __align__(16) float s_mem[];
+    float4* hs = reinterpret_cast<float4*>(s_mem);                              // [kChunk][Q][kThreads]: states, then their gradients
+    float* s_delta = s_mem + kChunk * SPT * kThreads;                           // [kChunk][CB] each
+    float *s_x = s_delta + kChunk * CB, *s_g = s_x + kChunk * CB, *s_gb = s_g + kChunk * CB, *s_gk = s_gb + kChunk * CB, *s_y = s_gk + kChunk * CB;
+    float(*sb)[SP] = reinterpret_cast<float(*)[SP]>(s_y + kChunk * CB);
+    float(*sc)[SP] = sb + kChunk;
+    uint8_t* fresh = reinterpret_cast<uint8_t*>(sc + kChunk);
+    pdl_wait();
+    pdl_trigger();
+    const int tid = threadIdx.x, across = (p.D + CB - 1) / CB, cb = (int)(blockIdx.x % across);
+    const int n = (int)(blockIdx.x / across % p.N), run = (int)(blockIdx.x / across / p.N);
+    const int sub = tid % LS, cl = tid / LS, s0 = sub * SPT, own = cb * CB + cl;
+    const bool on = own < p.D;
+    const int ch = on ? own : 0, channels = min(CB, p.D - cb * CB);
+    const int end = steps_of(p.lengths, n, p.T);
+    const int t0 = min(run * p.length, end), t1 = min(t0 + p.length, end), chunks = (t1 - t0 + kChunk - 1) / kChunk;
+    // the channel whose inputs and outputs this thread converts: the same for all its items
+    const int ic = tid % CB, ich = min(cb * CB + ic, p.D - 1);
+    const bool ion = cb * CB + ic < p.D;
+    const float iskip = p.d ? p.d[ich] : 0.f, ibias = p.dt_bias ? p.dt_bias[ich] : 0.f;
+    const size_t row0 = (size_t)run * p.N + n;
+
+    f32x2 a2[SPT / 2], h[SPT / 2], carry[SPT / 2], da[SPT / 2];
+    load_decays<SPT>(p, ch, s0, on, a2);
+    load_states<SPT>(p, q.first, row0, ch, s0, on, h);
+    load_states<SPT>(p, q.incoming, row0, ch, s0, on, carry);
+#pragma unroll
+    for (int i = 0; i < SPT / 2; ++i) da[i] = both(0.f);
+    float dskip = 0.f, dbias = 0.f;
+    float4* checks = reinterpret_cast<float4*>(q.checks) + (size_t)blockIdx.x * q.chunks * Q * kThreads + tid;
+
+    auto advance = [&](int j, f32x2 (&h)[SPT / 2]) {                            // one step of the state
+        const int at = j * CB + cl;
+        const float delta = s_delta[at];
+        const f32x2 d2 = both(delta), u2 = both(delta * s_x[at]);
+        const bool st = fresh[j];
+#pragma unroll
+        for (int i = 0; i < SPT / 2; i += 2) {
+            const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 2 * i]);
+            if (st) h[i] = h[i + 1] = both(0.f);
+            h[i] = fma2(exp2_pair(mul2(d2, a2[i])), h[i], mul2(u2, bv.x));
+            h[i + 1] = fma2(exp2_pair(mul2(d2, a2[i + 1])), h[i + 1], mul2(u2, bv.y));
+        }
+    };
+    auto stage_starts = [&](int t) {
+        if (tid < kChunk) fresh[tid] = p.starts && t + tid < t1 ? p.starts[(size_t)(t + tid) * p.N + n] : 0;
+    };
+
+    for (int k = 0; k < chunks; ++k) {                                          // states at the chunks' first steps
+#pragma unroll
+        for (int i = 0; i < Q; ++i)
+            checks[(size_t)(k * Q + i) * kThreads] = make_float4(lane_of(h[2 * i], 0), lane_of(h[2 * i], 1), lane_of(h[2 * i + 1], 0), lane_of(h[2 * i + 1], 1));
+        if (k == chunks - 1) break;                                             // that one's steps come next
+        const int t = t0 + k * kChunk;
+        stage_bc<T, kChunk, SP, kThreads>(p, b, nullptr, n, t, t1, sb, sc);
+        stage_starts(t);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int e = tid + i * kThreads;
+            const size_t row = (size_t)(t + e / CB) * p.N + n;
+            const float raw = to_float(dt[row * p.ld_dt + ich]) + ibias;
+            s_delta[e] = ion ? (p.softplus ? softplus(raw) : raw) : 0.f;
+            s_x[e] = ion ? to_float(x[row * p.ld_x + ich]) : 0.f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) advance(j, h);
+        __syncthreads();
+    }
+
+    for (int k = chunks - 1; k >= 0; --k) {
+        const int t = t0 + k * kChunk;
+        stage_bc<T, kChunk, SP, kThreads>(p, b, c, n, t, t1, sb, sc);
+        stage_starts(t);
+        float slope_dt[ITEMS], slope_z[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {                                       // steps behind the end: nothing in, all kept
+            const int e = tid + i * kThreads;
+            const bool live = ion && t + e / CB < t1;
+            float delta = 0.f, xv = 0.f, g = 0.f;
+            slope_dt[i] = 1.f; slope_z[i] = 0.f;
+            if (live) {
+                const size_t row = (size_t)(t + e / CB) * p.N + n;
+                const float raw = to_float(dt[row * p.ld_dt + ich]) + ibias;
+                delta = p.softplus ? softplus(raw, &slope_dt[i]) : raw;
+                xv = to_float(x[row * p.ld_x + ich]);
+                g = to_float(dy[row * q.ld_dy + ich]);
+                if (z) {
+                    const float zv = to_float(z[row * p.ld_z + ich]), sg = sigmoid(zv);
+                    slope_z[i] = g * (sg * (1.f + zv * (1.f - sg)));
+                    g *= zv * sg;
+                }
+                dskip = fmaf(g, xv, dskip);
+            }
+            s_delta[e] = delta; s_x[e] = xv; s_g[e] = g;
+        }
+        f32x2 h0[SPT / 2];
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const float4 v = checks[(size_t)(k * Q + i) * kThreads];
+            h[2 * i] = h0[2 * i] = pair(v.x, v.y);
+            h[2 * i + 1] = h0[2 * i + 1] = pair(v.z, v.w);
+        }
+        __syncthreads();
+#pragma unroll 2
+        for (int j = 0; j < kChunk; ++j) {                                      // the chunk's states, and the sums over them
+            advance(j, h);
+            f32x2 acc = both(0.f);
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]);
+                acc = fma2(cv.x, h[2 * i], acc);
+                acc = fma2(cv.y, h[2 * i + 1], acc);
+                *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(h[2 * i], h[2 * i + 1]);
+            }
+            float v = lane_of(acc, 0) + lane_of(acc, 1);
+#pragma unroll
+            for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (sub == 0) s_y[j * CB + cl] = v;
+        }
+        __syncthreads();
+        // sums over the block's channels of weight x what hs holds, four states of a step to a thread and a share of the channels
+        auto over_channels = [&](auto weight, int half) {
+            constexpr int QUADS = kChunk * SP / 4, WAYS = QUADS >= kThreads ? 1 : kThreads / QUADS < 8 ? kThreads / QUADS : 8;
+            static_assert(QUADS * WAYS % 32 == 0 && QUADS * WAYS <= kThreads, "whole warps, one turn");
+            if (tid < QUADS * WAYS) {           // eight neighbouring lanes read eight neighbouring pieces of 16 bytes
+                const int way = tid % WAYS, lane = tid / WAYS % LS, i = tid / (WAYS * LS) % Q, j = tid / (WAYS * LS * Q), quad = lane * Q + i;
+                const int slot = (j * Q + i) * kThreads + lane;
+                f32x2 u = both(0.f), v = both(0.f);
+#pragma unroll 4
+                for (int l = way; l < channels; l += WAYS) {
+                    const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&hs[slot + l * LS]);
+                    const f32x2 f = both(weight(j * CB + l));
+                    u = fma2(f, w.x, u);
+                    v = fma2(f, w.y, v);
+                }
+                float r[4] = {lane_of(u, 0), lane_of(u, 1), lane_of(v, 0), lane_of(v, 1)};
+#pragma unroll
+                for (int o = 1; o < WAYS; o <<= 1)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) r[k] += __shfl_xor_sync(0xffffffffu, r[k], o);
+                if (way == 0 && t + j < t1)
+                    *reinterpret_cast<float4*>(q.part_bc + (((size_t)cb * p.T + t + j) * p.N + n) * (2 * SP) + half * SP + 4 * quad) = make_float4(r[0], r[1], r[2], r[3]);
+            }
+        };
+        over_channels([&](int at) { return s_g[at]; }, 1);
+        __syncthreads();
+#pragma unroll 2
+        for (int j = kChunk - 1; j >= 0; --j) {                                 // back over the chunk
+            const int at = j * CB + cl;
+            const float delta = s_delta[at];
+            const f32x2 d2 = both(delta), g2 = both(s_g[at]);
+            const bool st = fresh[j];
+            f32x2 gb = both(0.f), gk = both(0.f);
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]), bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 4 * i]);
+                ulonglong2 old = j ? *reinterpret_cast<const ulonglong2*>(&hs[((j - 1) * Q + i) * kThreads + tid]) : make_ulonglong2(h0[2 * i], h0[2 * i + 1]);
+                if (st) old = make_ulonglong2(0, 0);
+                const f32x2 c2[2] = {cv.x, cv.y}, b2[2] = {bv.x, bv.y}, o2[2] = {old.x, old.y};
+                f32x2 grad[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int w = 2 * i + e;
+                    const f32x2 decay = exp2_pair(mul2(d2, a2[w]));
+                    grad[e] = fma2(g2, c2[e], carry[w]);
+                    const f32x2 kept = mul2(grad[e], mul2(decay, o2[e]));
+                    gk = fma2(a2[w], kept, gk);
+                    da[w] = fma2(d2, kept, da[w]);
+                    gb = fma2(grad[e], b2[e], gb);
+                    carry[w] = st ? both(0.f) : mul2(decay, grad[e]);
+                }
+                *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(grad[0], grad[1]);
+            }
+            float vb = lane_of(gb, 0) + lane_of(gb, 1), vk = lane_of(gk, 0) + lane_of(gk, 1);
+#pragma unroll
+            for (int o = 1; o < LS; o <<= 1) { vb += __shfl_xor_sync(0xffffffffu, vb, o); vk += __shfl_xor_sync(0xffffffffu, vk, o); }
+            if (sub == 0) { s_gb[at] = vb; s_gk[at] = vk; }
+        }
+        __syncthreads();
+        over_channels([&](int at) { return s_delta[at] * s_x[at]; }, 0);
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int e = tid + i * kThreads;
+            if (ion && t + e / CB < t1) {
+                const size_t row = (size_t)(t + e / CB) * p.N + n;
+                const float xv = s_x[e], gb = s_gb[e];
+                const float dd = fmaf(xv, gb, s_gk[e] * (1.f / kLog2e)) * slope_dt[i];       // a2 is A log2(e)
+                dbias += dd;
+                if (dx) dx[row * q.ld_dx + ich] = from_float<T>(fmaf(s_delta[e], gb, iskip * s_g[e]));
+                if (ddt) ddt[row * q.ld_ddt + ich] = from_float<T>(dd);
+                if (dz) dz[row * q.ld_dz + ich] = from_float<T>(slope_z[i] * fmaf(iskip, xv, s_y[e]));
+            }
+        }
+        __syncthreads();
+    }
+
+    if (run == 0 && q.dstate_in) store_states<SPT>(p, q.dstate_in, n, ch, s0, on, carry);
+    if (q.part_ch) {
+        float* part = q.part_ch + row0 * ((size_t)p.D * p.S + 2 * p.D);
+        store_states<SPT>(p, part, 0, ch, s0, on, da);
+        s_gb[tid] = dskip;                                                      // chunks hold kThreads items at least
+        s_gk[tid] = dbias;
+        __syncthreads();
+        if (tid < CB && ion) {
+#pragma unroll
+            for (int i = 1; i < LS; ++i) { dskip += s_gb[tid + i * CB]; dbias += s_gk[tid + i * CB]; }
+            part[(size_t)p.D * p.S + ich] = dskip;
+            part[(size_t)p.D * p.S + p.D + ich] = dbias;
+        }
+    }
+}
+template <int SPT, int LS> constexpr size_t gradient_shared()
+{
+    return (size_t)(kChunk * SPT * kThreads + 6 * kChunk * (kThreads / LS) + 2 * kChunk * SPT * LS) * 4 + 16;
+}
+
+// dB and dC: the channel blocks' parts added in order.
+template <typename T>
+__global__ void __launch_bounds__(256) bc_kernel(const ScanArgs p, int sp, int across, const float* part, T* db, T* dc, int64_t ld_db, int64_t ld_dc)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int64_t rows = (int64_t)p.T * p.N, id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / (2 * sp);
+    if (row >= rows) return;
+    const int e = (int)(id % (2 * sp)), s = e % sp;
+    if (s >= p.S || (int)(row / p.N) >= steps_of(p.lengths, (int)(row % p.N), p.T)) return;
+    float v = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < across; ++i) v += part[((size_t)i * rows + row) * (2 * sp) + e];
+    T* out = e < sp ? db : dc;
+    if (out) out[row * (e < sp ? ld_db : ld_dc) + s] = from_float<T>(v);
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------------
+// States of a thread and lanes of a channel.
+struct Shape { int spt, ls; };
+Shape scan_shape(int S)
+{
+    if (S <= 4) return {4, 1};
+    if (S <= 8) return {8, 1};
+    return {16, S <= 16 ? 1 : S <= 32 ? 2 : 4};
+}
+Shape gradient_shape(int S)
+{
+    if (S <= 4) return {4, 1};
+    return {8, S <= 8 ? 1 : S <= 16 ? 2 : S <= 32 ? 4 : 8};
+}
+template <typename F>
+hts_status by_scan_shape(int S, F f)
+{
+    const Shape h = scan_shape(S);
+    if (h.spt == 4) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
+    if (h.spt == 8) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
+    if (h.ls == 1) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+    if (h.ls == 2) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
+}
+template <typename F>
+hts_status by_gradient_shape(int S, F f)
+{
+    const Shape h = gradient_shape(S);
+    if (h.spt == 4) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
+    if (h.ls == 1) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
+    if (h.ls == 2) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
+    if (h.ls == 4) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
+    return f(std::integral_constant<int, 8>(), std::integral_constant<int, 8>());
+}
+
+// Runs so that `blocks` blocks exist, of `least` steps at least and a multiple of the steps staged at once.
+void cut_runs(int T, int64_t base, int64_t blocks, int least, int* runs, int* length)
+{
+    const int64_t want = ceil_div(blocks, base);
+    int64_t l = ceil_div(ceil_div(T, want), kGroup) * kGroup;
+    if (l < least) l = least;
+    *runs = (int)ceil_div(T, l);
+    *length = *runs == 1 ? T : (int)l;
+}
+int64_t channel_blocks(int D, Shape h) { return ceil_div(D, kThreads / h.ls); }
+
+struct Plan {
+    Shape shape;
+    int64_t across;
+    int runs, length, chunks;
+    size_t ends, sums, back, broken, checks, part_bc, part_ch, bytes;           // offsets in the workspace
+};
+Plan plan(int T, int N, int D, int S, bool gradient)
+{
+    Plan q{};
+    q.shape = gradient ? gradient_shape(S) : scan_shape(S);
+    q.across = channel_blocks(D, q.shape);
+    cut_runs(T, q.across * N, (int64_t)kCoreSms * (gradient ? 4 : 6), gradient ? 4 * kChunk : 4 * kGroup, &q.runs, &q.length);
+    size_t at = 0;
+    auto take = [&](size_t floats) { const size_t was = at; at += round256(floats * 4); return was; };
+    const size_t states = (size_t)N * D * S;
+    if (q.runs > 1) {
+        q.ends = take(q.runs * states);
+        if (gradient) q.back = take(q.runs * states);
+        q.sums = take((size_t)q.runs * N * D);
+        q.broken = take((size_t)q.runs * N);
+    }
+    if (gradient) {
+        q.chunks = (q.length + kChunk - 1) / kChunk;
+        q.checks = take((size_t)q.runs * N * q.across * q.chunks * q.shape.spt * kThreads);
+        q.part_bc = take((size_t)q.across * T * N * 2 * q.shape.spt * q.shape.ls);
+        q.part_ch = take((size_t)q.runs * N * ((size_t)D * S + 2 * D));
+    }
+    q.bytes = at;
+    return q;
+}
+RunMaps maps_at(const Plan& q, void* workspace)
+{
+    char* w = (char*)workspace;
+    return {(float*)(w + q.ends), (float*)(w + q.sums), (float*)(w + q.back), (uint8_t*)(w + q.broken)};
+}
+ScanArgs scan_args(const hts_scan_desc& d, const hts_scan_inputs& in)
+{
+    ScanArgs p{};
+    p.T = d.T; p.N = d.N; p.D = d.channels; p.S = d.state; p.runs = 1; p.length = d.T;
+    p.ld_x = d.ld_x; p.ld_dt = d.ld_dt; p.ld_b = d.ld_b; p.ld_c = d.ld_c; p.ld_z = d.ld_z; p.ld_y = d.ld_y;
+    p.a = in.a; p.d = in.d; p.dt_bias = in.dt_bias; p.starts = in.starts; p.lengths = in.lengths; p.softplus = d.softplus != 0;
+    return p;
+}
+hts_status launch_compose(const ScanArgs& p, const float* state_in, const float* dstate_out, const RunMaps& m, bool back, cudaStream_t s)
+{
+    const int64_t blocks = ceil_div((int64_t)p.N * p.D * p.S, 256);
+    HTS_CUDA(launch_pdl(compose_kernel, dim3((unsigned)blocks, back ? 2 : 1), dim3(256), 0, s, p, state_in, dstate_out, m));
+    note_launch();
+    return HTS_OK;
+}
+
+template <typename T>
+hts_status forward(ScanArgs p, const hts_scan_inputs& in, T* y, float* state_out, void* workspace, cudaStream_t s)
+{
+    const Plan q = plan(p.T, p.N, p.D, p.S, false);
+    p.runs = q.runs; p.length = q.length;
+    const T *x = (const T*)in.x, *dt = (const T*)in.dt, *b = (const T*)in.b, *c = (const T*)in.c, *z = (const T*)in.z, *none = nullptr;
+    const unsigned row = (unsigned)(q.across * p.N);
+    return by_scan_shape(p.S, [&](auto spt, auto ls) {
+        constexpr int SPT = decltype(spt)::value, LS = decltype(ls)::value;
+        const float* first = in.state_in;
+        RunMaps m{};
+        if (q.runs > 1) {
+            m = maps_at(q, workspace);
+            HTS_CUDA(launch_pdl(scan_kernel<T, SPT, LS, MAPS>, dim3(row * (q.runs - 1)), dim3(kThreads), 0, s, p, x, dt, b, c, z, none, (const float*)nullptr, (T*)nullptr,
+                                (float*)nullptr, m));
+            note_launch();
+            const hts_status st = launch_compose(p, in.state_in, nullptr, m, false, s);
+            if (st != HTS_OK) return st;
+            first = m.ends;
+        }
+        HTS_CUDA(launch_pdl(scan_kernel<T, SPT, LS, SCAN>, dim3(row * q.runs), dim3(kThreads), 0, s, p, x, dt, b, c, z, none, first, y, state_out, m));
+        note_launch();
+        return HTS_OK;
+    });
+}
+
+template <typename T>
+hts_status step(const ScanArgs& p, const hts_scan_inputs& in, const int32_t* slots, int pool, T* y, float* state_out, cudaStream_t s)
+{
+    const bool quads = p.S % 4 == 0 && aligned_to(in.state_in, 16) && aligned_to(state_out, 16) && aligned_to(in.a, 16);
+    const T *x = (const T*)in.x, *dt = (const T*)in.dt, *b = (const T*)in.b, *c = (const T*)in.c, *z = (const T*)in.z;
+    auto go = [&](auto ls) {
+        constexpr int LS = decltype(ls)::value;
+        // four rows a thread where that leaves eight blocks on every SM
+        const bool many = (int64_t)p.N * p.D * LS / 4 >= (int64_t)kCoreSms * 1024;
+        const int64_t blocks = ceil_div((int64_t)(many ? (p.N + 3) / 4 : p.N) * p.D * LS, 128);
+        if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
+        auto kernel = many ? (quads ? scan_step_kernel<T, LS, true, 4> : scan_step_kernel<T, LS, false, 4>)
+                           : (quads ? scan_step_kernel<T, LS, true, 1> : scan_step_kernel<T, LS, false, 1>);
+        HTS_CUDA(launch_pdl(kernel, dim3((unsigned)blocks), dim3(128), 0, s, p, x, dt, b, c, z, slots, pool, in.state_in, y, state_out));
+        note_launch();
+        return HTS_OK;
+    };
+    if (p.S <= 4) return go(std::integral_constant<int, 1>());
+    if (p.S <= 8) return go(std::integral_constant<int, 2>());
+    if (p.S <= 16) return go(std::integral_constant<int, 4>());
+    if (p.S <= 32) return go(std::integral_constant<int, 8>());
+    return go(std::integral_constant<int, 16>());
+}
+
+template <typename T>
+hts_status gradient(ScanArgs p, const hts_scan_inputs& in, const T* dy, int64_t ld_dy, const float* dstate_out, const hts_scan_grads& out, void* workspace, cudaStream_t s)
+{
+    const Plan q = plan(p.T, p.N, p.D, p.S, true);
+    p.runs = q.runs; p.length = q.length;
+    const T *x = (const T*)in.x, *dt = (const T*)in.dt, *b = (const T*)in.b, *c = (const T*)in.c, *z = (const T*)in.z;
+    const unsigned row = (unsigned)(q.across * p.N);
+    char* w = (char*)workspace;
+    const bool sums = out.a || out.d || out.dt_bias;
+    GradArgs g{ld_dy, out.ld_x, out.ld_dt, out.ld_z, (float*)(w + q.checks), (float*)(w + q.part_bc), sums ? (float*)(w + q.part_ch) : nullptr, in.state_in, dstate_out,
+               out.state_in, q.chunks};
+    if (q.runs > 1) {
+        const RunMaps m = maps_at(q, workspace);
+        ScanArgs e = p;
+        e.ld_y = ld_dy;
+        const hts_status st = by_scan_shape(p.S, [&](auto spt, auto ls) {
+            constexpr int SPT = decltype(spt)::value, LS = decltype(ls)::value;
+            const unsigned blocks = (unsigned)(channel_blocks(p.D, {SPT, LS}) * p.N * q.runs);
+            HTS_CUDA(launch_pdl(scan_kernel<T, SPT, LS, MAPS_BACK>, dim3(blocks), dim3(kThreads), 0, s, e, x, dt, b, c, z, dy, (const float*)nullptr, (T*)nullptr,
+                                (float*)nullptr, m));
+            note_launch();
+            return launch_compose(p, in.state_in, dstate_out, m, true, s);
+        });
+        if (st != HTS_OK) return st;
+        g.first = m.ends;
+        g.incoming = m.back;
+    }
+    hts_status st = by_gradient_shape(p.S, [&](auto spt, auto ls) {
+        constexpr int SPT = decltype(spt)::value, LS = decltype(ls)::value;
+        static OncePerDevice allowed;
+        HTS_CUDA(allow_shared(scan_gradient_kernel<T, SPT, LS>, allowed));
+        HTS_CUDA(launch_pdl(scan_gradient_kernel<T, SPT, LS>, dim3(row * q.runs), dim3(kThreads), gradient_shared<SPT, LS>(), s, p, g, x, dt, b, c, z, dy, (T*)out.x,
+                            (T*)out.dt, (T*)out.z));
+        note_launch();
+        return HTS_OK;
+    });
+    if (st != HTS_OK) return st;
+    if (out.b || out.c) {
+        const int sp = q.shape.spt * q.shape.ls;
+        const int64_t blocks = ceil_div((int64_t)p.T * p.N * 2 * sp, 256);
+        HTS_CUDA(launch_pdl(bc_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, p, sp, (int)q.across, (const float*)g.part_bc, (T*)out.b, (T*)out.c, out.ld_b, out.ld_c));
+        note_launch();
+    }
+    if (!sums) return HTS_OK;
+    const int64_t states = (int64_t)p.D * p.S;
+    return launch_column_sums({g.part_ch, (int64_t)q.runs * p.N, states + 2 * p.D, states, states, 1, out.a, out.d, states + p.D, out.dt_bias}, s);
+}
+
+// Blocks of one launch, of every kind: a grid has fewer than 2^31.
+bool too_many(int64_t T, int64_t N, int64_t D)
+{
+    return T * N > ((int64_t)1 << 31) || N * D > ((int64_t)1 << 31) || ceil_div(D, 16) * N * ceil_div(T, 32) > INT32_MAX;
+}
+bool bad(const hts_scan_desc* d, const hts_scan_inputs* in, bool with_steps)
+{
+    return !d || !in || (with_steps && d->T < 1) || d->N < 1 || d->channels < 1 || d->state < 1 || d->state > 64 ||
+           (d->dtype != HTS_DTYPE_FP32 && d->dtype != HTS_DTYPE_BF16) || !in->x || !in->dt || !in->a || !in->b || !in->c || d->ld_x < d->channels ||
+           d->ld_dt < d->channels || d->ld_b < d->state || d->ld_c < d->state || (in->z && d->ld_z < d->channels) || too_many(with_steps ? d->T : 1, d->N, d->channels);
+}
+
+}  // namespace
+}  // namespace hts
+
+using namespace hts;
+
+extern "C" int64_t hts_selective_scan_workspace(int32_t T, int32_t N, int32_t channels, int32_t state, int32_t gradient)
+{
+    if (T < 1 || N < 1 || channels < 1 || state < 1 || state > 64 || too_many(T, N, channels)) return 0;
+    return (int64_t)plan(T, N, channels, state, gradient != 0).bytes;
+}
+
+extern "C" hts_status hts_selective_scan(const hts_scan_desc* d, const hts_scan_inputs* in, void* y, float* state_out, void* workspace, int64_t workspace_bytes,
+                                         void* stream)
+{
+    if (bad(d, in, true) || !y || d->ld_y < d->channels || y == in->x || y == in->dt || y == in->z || (state_out && state_out == in->state_in)) return HTS_ERR_INVALID_ARG;
+    const int64_t need = hts_selective_scan_workspace(d->T, d->N, d->channels, d->state, 0);
+    if (need && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return HTS_ERR_INVALID_ARG;
+    const ScanArgs p = scan_args(*d, *in);
+    if (d->dtype == HTS_DTYPE_FP32) return forward(p, *in, (float*)y, state_out, workspace, (cudaStream_t)stream);
+    return forward(p, *in, (__nv_bfloat16*)y, state_out, workspace, (cudaStream_t)stream);
+}
+
+extern "C" hts_status hts_selective_scan_step(const hts_scan_desc* d, const hts_scan_inputs* in, const int32_t* slots, int32_t pool, void* y, float* state_out, void* stream)
+{
+    if (bad(d, in, false) || !y || !in->state_in || !state_out || in->lengths || d->ld_y < d->channels || y == in->x || y == in->dt || y == in->z || pool < 1 ||
+        (!slots && pool < d->N))
+        return HTS_ERR_INVALID_ARG;
+    const ScanArgs p = scan_args(*d, *in);
+    if (d->dtype == HTS_DTYPE_FP32) return step(p, *in, slots, pool, (float*)y, state_out, (cudaStream_t)stream);
+    return step(p, *in, slots, pool, (__nv_bfloat16*)y, state_out, (cudaStream_t)stream);
+}
+
+extern "C" hts_status hts_selective_scan_gradient(const hts_scan_desc* d, const hts_scan_inputs* in, const void* dy, int64_t ld_dy, const float* dstate_out,
+                                                  const hts_scan_grads* out, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (bad(d, in, true) || !dy || ld_dy < d->channels || !out || (out->x && out->ld_x < d->channels) || (out->dt && out->ld_dt < d->channels) ||
+        (out->z && (out->ld_z < d->channels || !in->z)) || (out->b && out->ld_b < d->state) || (out->c && out->ld_c < d->state))
+        return HTS_ERR_INVALID_ARG;
+    if (!out->x && !out->dt && !out->a && !out->b && !out->c && !out->d && !out->dt_bias && !out->z && !out->state_in) return HTS_ERR_INVALID_ARG;
+    for (const void* o : {out->x, out->dt, out->z, out->b, out->c})
+        if (o && (o == in->x || o == in->dt || o == in->z || o == in->b || o == in->c || o == dy)) return HTS_ERR_INVALID_ARG;
+    if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < hts_selective_scan_workspace(d->T, d->N, d->channels, d->state, 1)) return HTS_ERR_INVALID_ARG;
+    const ScanArgs p = scan_args(*d, *in);
+    if (d->dtype == HTS_DTYPE_FP32) return gradient(p, *in, (const float*)dy, ld_dy, dstate_out, *out, workspace, (cudaStream_t)stream);
+    return gradient(p, *in, (const __nv_bfloat16*)dy, ld_dy, dstate_out, *out, workspace, (cudaStream_t)stream);
+}
