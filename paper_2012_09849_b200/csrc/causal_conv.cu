@@ -12,8 +12,8 @@
 namespace hts {
 namespace {
 
-constexpr int kVector = 4;                      // channels of a thread where alignment allows, else one
-constexpr int kWarps = 8, kGroup = 8;           // warps of a block (a run each); steps loaded at once
+constexpr int kVector = 4, kGradVector = 2;     // channels of a thread where alignment allows, else one
+constexpr int kWarps = 8, kGroup = 4;           // warps of a block (a run each); steps loaded at once
 
 struct ConvArgs {
     int T, N, D, lanes, runs, length;           // lanes: vectors of channels; runs per sequence, of `length` steps
@@ -102,7 +102,7 @@ __device__ __forceinline__ void weights(const ConvArgs& p, int c, float (&w)[W][
 }
 
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(32 * kWarps) conv_kernel(const ConvArgs p, const T* x, const T* window_in, T* y, T* window_out)
+__global__ void __launch_bounds__(32 * kWarps, 4) conv_kernel(const ConvArgs p, const T* x, const T* window_in, T* y, T* window_out)
 {
     pdl_wait();
     pdl_trigger();
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const ConvArgs p, const 
 // A run walks W - 1 steps past its end, for the terms that those steps add to its inputs' gradients.  `pend[j]`: the gradient
 // of the input W - 1 - j steps back, complete when it reaches j = 0.  part: [block of runs][W + 1][D], weights then bias.
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(32 * kWarps) conv_gradient_kernel(const ConvArgs p, const T* x, const T* window_in, const T* dy, const float* dwindow_out,
+__global__ void __launch_bounds__(32 * kWarps, 4) conv_gradient_kernel(const ConvArgs p, const T* x, const T* window_in, const T* dy, const float* dwindow_out,
                                                                     T* dx, float* dwindow_in, float* part)
 {
     pdl_wait();
@@ -316,11 +316,11 @@ void cut_runs(ConvArgs& p, int V, int least)
 }
 int64_t run_blocks(const ConvArgs& p) { return ceil_div((int64_t)p.N * p.runs, kWarps); }
 // Whether vectors of channels of every tensor start on a boundary of their own size.
-bool vectors(int64_t D, size_t bytes, std::initializer_list<const void*> pointers, std::initializer_list<int64_t> strides)
+bool vectors(int64_t D, size_t bytes, std::initializer_list<const void*> pointers, std::initializer_list<int64_t> strides, int V = kVector)
 {
-    bool ok = D % kVector == 0;
+    bool ok = D % V == 0;
     for (const void* q : pointers) ok = ok && aligned_to(q, bytes);
-    for (int64_t l : strides) ok = ok && l % kVector == 0;
+    for (int64_t l : strides) ok = ok && l % V == 0;
     return ok;
 }
 
@@ -375,14 +375,15 @@ template <typename T>
 hts_status gradient(ConvArgs p, int width, const T* x, const T* win, const T* dy, const float* dwout, T* dx, float* dw, float* db, float* dwin, float* part,
                     cudaStream_t s)
 {
-    const bool wide = vectors(p.D, kVector * sizeof(T), {x, win, dy, dx}, {p.ld_x, p.ld_dy, dx ? p.ld_dx : 0}) && aligned_to(dwin, 16);
-    cut_runs(p, wide ? kVector : 1, kGradientRun);
+    const bool wide = vectors(p.D, kGradVector * sizeof(T), {x, win, dy, dx}, {p.ld_x, p.ld_dy, dx ? p.ld_dx : 0}, kGradVector) &&
+                      aligned_to(dwin, kGradVector * sizeof(float));
+    cut_runs(p, wide ? kGradVector : 1, kGradientRun);
     const int64_t rows = run_blocks(p), blocks = rows * ceil_div(p.lanes, 32);
     if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
     const bool sums = dw || db;
     const hts_status st = by_width(width, [&](auto k) {
         constexpr int W = decltype(k)::value;
-        HTS_CUDA(launch_pdl(wide ? conv_gradient_kernel<T, kVector, W> : conv_gradient_kernel<T, 1, W>, dim3((unsigned)blocks), dim3(32, kWarps), 0, s, p, x, win, dy,
+        HTS_CUDA(launch_pdl(wide ? conv_gradient_kernel<T, kGradVector, W> : conv_gradient_kernel<T, 1, W>, dim3((unsigned)blocks), dim3(32, kWarps), 0, s, p, x, win, dy,
                             dwout, dx, dwin, sums ? part : nullptr));
         note_launch();
         return HTS_OK;
@@ -415,7 +416,7 @@ extern "C" int64_t hts_causal_conv_workspace(int32_t T, int32_t N, int32_t chann
 {
     if (T < 1 || N < 1 || channels < 1 || width < 2 || width > 4) return 0;
     int64_t rows = 0;
-    for (int V : {1, kVector}) {                // whichever form the pointers' alignment allows
+    for (int V : {1, kGradVector}) {                // whichever form the pointers' alignment allows
         if (channels % V) continue;
         ConvArgs p{};
         p.T = T; p.N = N; p.D = channels;

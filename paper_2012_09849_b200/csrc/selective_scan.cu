@@ -57,7 +57,43 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-__device__ __forceinline__ f32x2 exp2_pair(f32x2 v) { return pair(exp2_approx(lane_of(v, 0)), exp2_approx(lane_of(v, 1))); }
+// 2^v without the special-function unit, which every state's decay would otherwise wait for (sixteen results per SM and clock against
+// 128 multiply-adds): v = i + f with |f| <= 1/2, a polynomial of degree 5 in f, i added to the exponent.  |v| < 125.  The coefficients
+// are a least-maximum fit of (2^f - 1) / 2^f over |f| + 0.03, so that a decay near 1, which acts for many steps, is as exact as
+// its rounding and not off in one direction: mean error below 5e-10 for -0.06 < v < 0, ex2.approx -2e-8.
+__device__ __forceinline__ f32x2 exp2_poly(f32x2 v)
+{
+    const f32x2 t = fma2(v, both(1.f), both(12582912.f)), i = fma2(t, both(1.f), both(-12582912.f)), f = fma2(i, both(-1.f), v);
+    f32x2 r = fma2(both(0.0013266360620036721f), f, both(0.00966658629477024f));
+    r = fma2(r, f, both(0.05550675094127655f));
+    r = fma2(r, f, both(0.24022343754768372f));
+    r = fma2(r, f, both(0.6931470632553101f));
+    r = fma2(r, f, both(1.f));
+    return pair(__int_as_float(__float_as_int(lane_of(r, 0)) + (__float_as_int(lane_of(t, 0)) << 23)),
+                __int_as_float(__float_as_int(lane_of(r, 1)) + (__float_as_int(lane_of(t, 1)) << 23)));
+}
+// 2^v of pair i of a thread's states; the first N pairs by the polynomial.
+template <int N>
+__device__ __forceinline__ f32x2 exp2_pair(f32x2 v, int i)
+{
+    return i < N ? exp2_poly(v) : pair(exp2_approx(lane_of(v, 0)), exp2_approx(lane_of(v, 1)));
+}
+// f(N) where the first N pairs' exponents are small, else f(0): once per step, all pairs together.
+template <int N, typename F>
+__device__ __forceinline__ void by_size(bool small, F f)
+{
+    if (small) f(std::integral_constant<int, N>());
+    else f(std::integral_constant<int, 0>());
+}
+// |delta| below this: exponents of the first N pairs are below 125.  No delta is where an A is infinite or NaN.
+template <int N, int PAIRS>
+__device__ __forceinline__ float small_delta(const f32x2 (&a2)[PAIRS])
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum += fabsf(lane_of(a2[i], 0)) + fabsf(lane_of(a2[i], 1));
+    return 125.f / sum;
+}
 
 // log(1 + exp(v)) = max(v, 0) + log(1 + e), e = exp(-|v|); log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by atanh's power
 // series: the first term left out is below 2e-8 of the sum.  `slope`: its derivative.
@@ -122,6 +158,10 @@ __device__ __forceinline__ void stage_bc(const ScanArgs& p, const T* b, const T*
     }
 }
 
+// Pairs of a thread's states whose decays the multiply-adds compute.
+template <int SPT> constexpr int kScanPoly = SPT == 16 ? 3 : SPT == 8 ? 2 : 1;
+template <int SPT> constexpr int kGradientPoly = SPT == 8 ? 2 : 1;
+
 enum Mode { SCAN, MAPS, MAPS_BACK };            // outputs; the runs' maps; those and what the runs hand back
 
 // SPT states a thread, LS lanes a channel.  dy: MAPS_BACK only, in the place of y.
@@ -129,7 +169,7 @@ template <typename T, int SPT, int LS, Mode MODE>
 __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const T* x, const T* dt, const T* b, const T* c, const T* z, const T* dy, const float* first,
                                                         T* y, float* state_out, RunMaps m)
 {
-    constexpr int SP = SPT * LS, CB = kThreads / LS;
+    constexpr int SP = SPT * LS, CB = kThreads / LS, NP = kScanPoly<SPT>;
     __shared__ __align__(16) float sb[2][kGroup][SP], sc[2][kGroup][SP];
     __shared__ uint8_t fresh[2][kGroup];
     pdl_wait();
@@ -144,6 +184,7 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const 
 
     f32x2 a2[SPT / 2], h[SPT / 2], prod[SPT / 2], back[SPT / 2];
     load_decays<SPT>(p, ch, s0, on, a2);
+    const float limit = small_delta<NP>(a2);
     load_states<SPT>(p, MODE == SCAN ? first : nullptr, (size_t)run * p.N + n, ch, s0, on, h);
     if (MODE == MAPS_BACK)
 #pragma unroll
@@ -176,12 +217,14 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const 
             }
             sum += delta;
             const f32x2 d2 = both(delta), u2 = both(delta * xv);
+            const bool small = fabsf(delta) < limit;
             float g = 0.f;
             if (MODE == MAPS_BACK) {
                 g = to_float(rg[j]);
                 if (z) g *= silu(to_float(rz[j]));
             }
             f32x2 acc[2] = {both(0.f), both(0.f)};
+            by_size<NP>(small, [&](auto poly) {
 #pragma unroll
             for (int i = 0; i < SPT / 2; i += 2) {
                 const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[buf][j][s0 + 2 * i]);
@@ -193,7 +236,7 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const 
                 }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const f32x2 decay = exp2_pair(mul2(d2, a2[i + k]));
+                    const f32x2 decay = exp2_pair<decltype(poly)::value>(mul2(d2, a2[i + k]), i + k);
                     h[i + k] = fma2(decay, h[i + k], mul2(u2, bb[k]));
                     if (MODE == SCAN) acc[k] = fma2(cc[k], h[i + k], acc[k]);
                     if (MODE == MAPS_BACK && !broken) {
@@ -202,6 +245,7 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const 
                     }
                 }
             }
+            });
             if (MODE == SCAN) {
                 float v = (lane_of(acc[0], 0) + lane_of(acc[1], 0)) + (lane_of(acc[0], 1) + lane_of(acc[1], 1));
 #pragma unroll
@@ -300,12 +344,21 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const ScanArgs p, const 
         const int n = min(n0 + r, p.N - 1);
         const bool fresh = p.starts && p.starts[n];
         const float xv = to_float(x[(size_t)n * p.ld_x + ch]), raw = to_float(dt[(size_t)n * p.ld_dt + ch]) + bias, delta = p.softplus ? softplus(raw) : raw;
-        float v = 0.f;
+        float v = 0.f, bv[4], cv[4];
+        if (QUADS) {
+            const Vec<T, 4> rb = load_vec<4>(b + (size_t)n * p.ld_b + (s0 < p.S ? s0 : 0)), rc = load_vec<4>(c + (size_t)n * p.ld_c + (s0 < p.S ? s0 : 0));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { bv[i] = to_float(rb.v[i]); cv[i] = s0 < p.S ? to_float(rc.v[i]) : 0.f; }
+        } else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                bv[i] = s0 + i < p.S ? to_float(b[(size_t)n * p.ld_b + s0 + i]) : 0.f;
+                cv[i] = s0 + i < p.S ? to_float(c[(size_t)n * p.ld_c + s0 + i]) : 0.f;
+            }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float bv = s0 + i < p.S ? to_float(b[(size_t)n * p.ld_b + s0 + i]) : 0.f, cv = s0 + i < p.S ? to_float(c[(size_t)n * p.ld_c + s0 + i]) : 0.f;
-            h[r][i] = fmaf(exp2_approx(delta * a2[i]), fresh ? 0.f : h[r][i], delta * xv * bv);
-            v = fmaf(cv, h[r][i], v);
+            h[r][i] = fmaf(exp2_approx(delta * a2[i]), fresh ? 0.f : h[r][i], delta * xv * bv[i]);
+            v = fmaf(cv[i], h[r][i], v);
         }
 #pragma unroll
         for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -344,7 +397,7 @@ template <typename T, int SPT, int LS>
 __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs p, const GradArgs q, const T* x, const T* dt, const T* b, const T* c, const T* z,
                                                                  const T* dy, T* dx, T* ddt, T* dz)
 {
-    constexpr int SP = SPT * LS, CB = kThreads / LS, Q = SPT / 4, ITEMS = kChunk * CB / kThreads;
+    constexpr int SP = SPT * LS, CB = kThreads / LS, Q = SPT / 4, ITEMS = kChunk * CB / kThreads, NP = kGradientPoly<SPT>;
     extern __shared__ __align__(16) float s_mem[];
     float4* hs = reinterpret_cast<float4*>(s_mem);                              // [kChunk][Q][kThreads]: states, then their gradients
     float* s_delta = s_mem + kChunk * SPT * kThreads;                           // [kChunk][CB] each
@@ -369,6 +422,7 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
 
     f32x2 a2[SPT / 2], h[SPT / 2], carry[SPT / 2], da[SPT / 2];
     load_decays<SPT>(p, ch, s0, on, a2);
+    const float limit = small_delta<NP>(a2);
     load_states<SPT>(p, q.first, row0, ch, s0, on, h);
     load_states<SPT>(p, q.incoming, row0, ch, s0, on, carry);
 #pragma unroll
@@ -380,45 +434,82 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
         const int at = j * CB + cl;
         const float delta = s_delta[at];
         const f32x2 d2 = both(delta), u2 = both(delta * s_x[at]);
-        const bool st = fresh[j];
+        if (fresh[j])
 #pragma unroll
-        for (int i = 0; i < SPT / 2; i += 2) {
-            const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 2 * i]);
-            if (st) h[i] = h[i + 1] = both(0.f);
-            h[i] = fma2(exp2_pair(mul2(d2, a2[i])), h[i], mul2(u2, bv.x));
-            h[i + 1] = fma2(exp2_pair(mul2(d2, a2[i + 1])), h[i + 1], mul2(u2, bv.y));
-        }
+            for (int i = 0; i < SPT / 2; ++i) h[i] = both(0.f);
+        by_size<NP>(fabsf(delta) < limit, [&](auto poly) {
+#pragma unroll
+            for (int i = 0; i < SPT / 2; i += 2) {
+                const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 2 * i]);
+                h[i] = fma2(exp2_pair<decltype(poly)::value>(mul2(d2, a2[i]), i), h[i], mul2(u2, bv.x));
+                h[i + 1] = fma2(exp2_pair<decltype(poly)::value>(mul2(d2, a2[i + 1]), i + 1), h[i + 1], mul2(u2, bv.y));
+            }
+        });
     };
-    auto stage_starts = [&](int t) {
-        if (tid < kChunk) fresh[tid] = p.starts && t + tid < t1 ? p.starts[(size_t)(t + tid) * p.N + n] : 0;
+    // A chunk's inputs as they lie in memory: asked for while the chunk before is worked on.
+    constexpr int BC = (kChunk * SP + kThreads - 1) / kThreads;
+    T rx[ITEMS], rdt[ITEMS], rg[ITEMS], rz[ITEMS], rb[BC], rc[BC];
+    uint8_t rst = 0;
+    const int first_row = tid / CB, rows_apart = kThreads / CB;
+    auto ask = [&](int t, bool all) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const size_t row = (size_t)min(t + first_row + i * rows_apart, t1 - 1) * p.N + n;
+            rdt[i] = dt[row * p.ld_dt + ich];
+            rx[i] = x[row * p.ld_x + ich];
+            if (all) rg[i] = dy[row * q.ld_dy + ich];
+            if (all && z) rz[i] = z[row * p.ld_z + ich];
+        }
+#pragma unroll
+        for (int i = 0; i < BC; ++i) {
+            const int e = tid + i * kThreads, s = min(e % SP, p.S - 1);
+            const size_t row = (size_t)min(t + e / SP, t1 - 1) * p.N + n;
+            rb[i] = b[row * p.ld_b + s];
+            if (all) rc[i] = c[row * p.ld_c + s];
+        }
+        if (tid < kChunk) rst = p.starts ? p.starts[(size_t)min(t + tid, t1 - 1) * p.N + n] : 0;
+    };
+    auto stage_bc_starts = [&](int t, bool all) {                               // zero behind the last state and step
+#pragma unroll
+        for (int i = 0; i < BC; ++i) {
+            const int e = tid + i * kThreads, j = e / SP, s = e % SP;
+            if (kChunk * SP % kThreads && e >= kChunk * SP) break;
+            const bool live = s < p.S && t + j < t1;
+            sb[j][s] = live ? to_float(rb[i]) : 0.f;
+            if (all) sc[j][s] = live ? to_float(rc[i]) : 0.f;
+        }
+        if (tid < kChunk) fresh[tid] = t + tid < t1 ? rst : 0;
     };
 
+    if (chunks > 1) ask(t0, false);
     for (int k = 0; k < chunks; ++k) {                                          // states at the chunks' first steps
 #pragma unroll
         for (int i = 0; i < Q; ++i)
             checks[(size_t)(k * Q + i) * kThreads] = make_float4(lane_of(h[2 * i], 0), lane_of(h[2 * i], 1), lane_of(h[2 * i + 1], 0), lane_of(h[2 * i + 1], 1));
         if (k == chunks - 1) break;                                             // that one's steps come next
         const int t = t0 + k * kChunk;
-        stage_bc<T, kChunk, SP, kThreads>(p, b, nullptr, n, t, t1, sb, sc);
-        stage_starts(t);
+        stage_bc_starts(t, false);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int e = tid + i * kThreads;
-            const size_t row = (size_t)(t + e / CB) * p.N + n;
-            const float raw = to_float(dt[row * p.ld_dt + ich]) + ibias;
+            const float raw = to_float(rdt[i]) + ibias;
             s_delta[e] = ion ? (p.softplus ? softplus(raw) : raw) : 0.f;
-            s_x[e] = ion ? to_float(x[row * p.ld_x + ich]) : 0.f;
+            s_x[e] = ion ? to_float(rx[i]) : 0.f;
         }
         __syncthreads();
+        ask(t + kChunk, k + 2 >= chunks);
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) advance(j, h);
         __syncthreads();
     }
+    if (chunks == 1) ask(t0, true);
 
+    f32x2 ahead[SPT / 2];                                                       // the next chunk's first state
+#pragma unroll
+    for (int i = 0; i < SPT / 2; ++i) ahead[i] = h[i];
     for (int k = chunks - 1; k >= 0; --k) {
         const int t = t0 + k * kChunk;
-        stage_bc<T, kChunk, SP, kThreads>(p, b, c, n, t, t1, sb, sc);
-        stage_starts(t);
+        stage_bc_starts(t, true);
         float slope_dt[ITEMS], slope_z[ITEMS];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {                                       // steps behind the end: nothing in, all kept
@@ -427,13 +518,12 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
             float delta = 0.f, xv = 0.f, g = 0.f;
             slope_dt[i] = 1.f; slope_z[i] = 0.f;
             if (live) {
-                const size_t row = (size_t)(t + e / CB) * p.N + n;
-                const float raw = to_float(dt[row * p.ld_dt + ich]) + ibias;
+                const float raw = to_float(rdt[i]) + ibias;
                 delta = p.softplus ? softplus(raw, &slope_dt[i]) : raw;
-                xv = to_float(x[row * p.ld_x + ich]);
-                g = to_float(dy[row * q.ld_dy + ich]);
+                xv = to_float(rx[i]);
+                g = to_float(rg[i]);
                 if (z) {
-                    const float zv = to_float(z[row * p.ld_z + ich]), sg = sigmoid(zv);
+                    const float zv = to_float(rz[i]), sg = sigmoid(zv);
                     slope_z[i] = g * (sg * (1.f + zv * (1.f - sg)));
                     g *= zv * sg;
                 }
@@ -443,12 +533,17 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
         }
         f32x2 h0[SPT / 2];
 #pragma unroll
-        for (int i = 0; i < Q; ++i) {
-            const float4 v = checks[(size_t)(k * Q + i) * kThreads];
-            h[2 * i] = h0[2 * i] = pair(v.x, v.y);
-            h[2 * i + 1] = h0[2 * i + 1] = pair(v.z, v.w);
-        }
+        for (int i = 0; i < SPT / 2; ++i) h[i] = h0[i] = ahead[i];
         __syncthreads();
+        if (k) {
+            ask(t - kChunk, true);
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                const float4 v = checks[(size_t)((k - 1) * Q + i) * kThreads];
+                ahead[2 * i] = pair(v.x, v.y);
+                ahead[2 * i + 1] = pair(v.z, v.w);
+            }
+        }
 #pragma unroll 2
         for (int j = 0; j < kChunk; ++j) {                                      // the chunk's states, and the sums over them
             advance(j, h);
@@ -497,8 +592,9 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
             const int at = j * CB + cl;
             const float delta = s_delta[at];
             const f32x2 d2 = both(delta), g2 = both(s_g[at]);
-            const bool st = fresh[j];
+            const bool st = fresh[j], small = fabsf(delta) < limit;
             f32x2 gb = both(0.f), gk = both(0.f);
+            by_size<NP>(small, [&](auto poly) {
 #pragma unroll
             for (int i = 0; i < Q; ++i) {
                 const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]), bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 4 * i]);
@@ -509,7 +605,7 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int w = 2 * i + e;
-                    const f32x2 decay = exp2_pair(mul2(d2, a2[w]));
+                    const f32x2 decay = exp2_pair<decltype(poly)::value>(mul2(d2, a2[w]), w);
                     grad[e] = fma2(g2, c2[e], carry[w]);
                     const f32x2 kept = mul2(grad[e], mul2(decay, o2[e]));
                     gk = fma2(a2[w], kept, gk);
@@ -519,6 +615,7 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
                 }
                 *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(grad[0], grad[1]);
             }
+            });
             float vb = lane_of(gb, 0) + lane_of(gb, 1), vk = lane_of(gk, 0) + lane_of(gk, 1);
 #pragma unroll
             for (int o = 1; o < LS; o <<= 1) { vb += __shfl_xor_sync(0xffffffffu, vb, o); vk += __shfl_xor_sync(0xffffffffu, vk, o); }
@@ -705,7 +802,8 @@ hts_status forward(ScanArgs p, const hts_scan_inputs& in, T* y, float* state_out
 template <typename T>
 hts_status step(const ScanArgs& p, const hts_scan_inputs& in, const int32_t* slots, int pool, T* y, float* state_out, cudaStream_t s)
 {
-    const bool quads = p.S % 4 == 0 && aligned_to(in.state_in, 16) && aligned_to(state_out, 16) && aligned_to(in.a, 16);
+    const bool quads = p.S % 4 == 0 && aligned_to(in.state_in, 16) && aligned_to(state_out, 16) && aligned_to(in.a, 16) && aligned_to(in.b, 4 * sizeof(T)) &&
+                       aligned_to(in.c, 4 * sizeof(T)) && p.ld_b % 4 == 0 && p.ld_c % 4 == 0;
     const T *x = (const T*)in.x, *dt = (const T*)in.dt, *b = (const T*)in.b, *c = (const T*)in.c, *z = (const T*)in.z;
     auto go = [&](auto ls) {
         constexpr int LS = decltype(ls)::value;
