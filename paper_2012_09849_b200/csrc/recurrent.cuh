@@ -43,8 +43,30 @@ __device__ __forceinline__ void store_vec(T* p, const float (&f)[V])
     *reinterpret_cast<Vec<T, V>*>(p) = r;
 }
 
+__device__ __forceinline__ void copy16(void* smem, const void* from, bool on)       // 16 bytes on their way to shared memory, zeros if not `on`
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(from), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+
+// 2^v and 1 / v without the steps that scale subnormal numbers: those count as zero here.
+__device__ __forceinline__ float exp2_approx(float v)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float rcp_approx(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+
 // 1 / (1 + exp(-v)): 0 and 1 at the infinities
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+__device__ __forceinline__ float sigmoid(float v) { return rcp_approx(1.f + exp2_approx(-kLog2e * v)); }
 __device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
 __device__ __forceinline__ float silu_slope(float v)
 {

@@ -21,7 +21,7 @@ namespace hts {
 namespace {
 
 constexpr int kThreads = 128, kGroup = 8;       // threads of a block; steps staged at once
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kStages = 2;                      // groups of steps in shared memory
 
 struct ScanArgs {
     int T, N, D, S;
@@ -39,12 +39,6 @@ struct RunMaps {
     uint8_t* broken;
 };
 
-__device__ __forceinline__ float exp2_approx(float v)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
 {
     f32x2 r;
@@ -57,49 +51,21 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-// 2^v without the special-function unit, which every state's decay would otherwise wait for (sixteen results per SM and clock against
-// 128 multiply-adds): v = i + f with |f| <= 1/2, a polynomial of degree 5 in f, i added to the exponent.  |v| < 125.  The coefficients
-// are a least-maximum fit of (2^f - 1) / 2^f over |f| + 0.03, so that a decay near 1, which acts for many steps, is as exact as
-// its rounding and not off in one direction: mean error below 5e-10 for -0.06 < v < 0, ex2.approx -2e-8.
-__device__ __forceinline__ f32x2 exp2_poly(f32x2 v)
+// exp(delta A) of a pair of states, a2 = A log2(e).  ex2.approx comes out 2e-8 too small on average for exponents between -1 and 0
+// (a third of a last place; measured over each part of that range), and a decay near 1 acts for hundreds of steps, so that the
+// sums drift: states of a 128-step rollout off by 2.1e-6.  Adding 2.3e-8 to the exponent, in the multiply-add that forms it, takes
+// the mean out (it is within 5e-9): 0.5e-6.
+__device__ __forceinline__ f32x2 decay_pair(f32x2 delta, f32x2 a2)
 {
-    const f32x2 t = fma2(v, both(1.f), both(12582912.f)), i = fma2(t, both(1.f), both(-12582912.f)), f = fma2(i, both(-1.f), v);
-    f32x2 r = fma2(both(0.0013266360620036721f), f, both(0.00966658629477024f));
-    r = fma2(r, f, both(0.05550675094127655f));
-    r = fma2(r, f, both(0.24022343754768372f));
-    r = fma2(r, f, both(0.6931470632553101f));
-    r = fma2(r, f, both(1.f));
-    return pair(__int_as_float(__float_as_int(lane_of(r, 0)) + (__float_as_int(lane_of(t, 0)) << 23)),
-                __int_as_float(__float_as_int(lane_of(r, 1)) + (__float_as_int(lane_of(t, 1)) << 23)));
-}
-// 2^v of pair i of a thread's states; the first N pairs by the polynomial.
-template <int N>
-__device__ __forceinline__ f32x2 exp2_pair(f32x2 v, int i)
-{
-    return i < N ? exp2_poly(v) : pair(exp2_approx(lane_of(v, 0)), exp2_approx(lane_of(v, 1)));
-}
-// f(N) where the first N pairs' exponents are small, else f(0): once per step, all pairs together.
-template <int N, typename F>
-__device__ __forceinline__ void by_size(bool small, F f)
-{
-    if (small) f(std::integral_constant<int, N>());
-    else f(std::integral_constant<int, 0>());
-}
-// |delta| below this: exponents of the first N pairs are below 125.  No delta is where an A is infinite or NaN.
-template <int N, int PAIRS>
-__device__ __forceinline__ float small_delta(const f32x2 (&a2)[PAIRS])
-{
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum += fabsf(lane_of(a2[i], 0)) + fabsf(lane_of(a2[i], 1));
-    return 125.f / sum;
+    const f32x2 v = fma2(delta, a2, both(2.3e-8f));
+    return pair(exp2_approx(lane_of(v, 0)), exp2_approx(lane_of(v, 1)));
 }
 
 // log(1 + exp(v)) = max(v, 0) + log(1 + e), e = exp(-|v|); log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by atanh's power
 // series: the first term left out is below 2e-8 of the sum.  `slope`: its derivative.
 __device__ __forceinline__ float softplus(float v, float* slope = nullptr)
 {
-    const float e = __expf(-fabsf(v)), s = __fdividef(e, 2.f + e), q = s * s;
+    const float e = exp2_approx(-kLog2e * fabsf(v)), s = e * rcp_approx(2.f + e), q = s * s;
     float r = 1.f / 13.f;
     r = fmaf(r, q, 1.f / 11.f);
     r = fmaf(r, q, 1.f / 9.f);
@@ -107,10 +73,19 @@ __device__ __forceinline__ float softplus(float v, float* slope = nullptr)
     r = fmaf(r, q, 1.f / 5.f);
     r = fmaf(r, q, 1.f / 3.f);
     r = fmaf(r, q, 1.f);
-    if (slope) *slope = __fdividef(v >= 0.f ? 1.f : e, 1.f + e);
+    if (slope) *slope = (v >= 0.f ? 1.f : e) * rcp_approx(1.f + e);
     return fmaxf(v, 0.f) + 2.f * s * r;
 }
 __device__ __forceinline__ int steps_of(const int32_t* lengths, int n, int T) { return lengths ? min(max(lengths[n], 0), T) : T; }
+
+// A value that every lane of the warp has, where the compiler can see it: addresses that depend on it alone are computed once per warp.
+__device__ __forceinline__ int uniform(int v) { return __reduce_min_sync(0xffffffffu, v); }
+// Lane j's part of which of the steps t .. t + 7 begin an episode; __ballot_sync makes a bit each of them, later.
+__device__ __forceinline__ uint8_t start_at(const ScanArgs& p, int n, int t, int end)
+{
+    const int lane = threadIdx.x & 31, at = t + lane;
+    return p.starts && lane < 8 && at < end ? p.starts[(size_t)at * p.N + n] : 0;
+}
 
 // SP states of A, times log2(e), as pairs; zero behind the last state.
 template <int SP>
@@ -143,35 +118,35 @@ __device__ __forceinline__ void store_states(const ScanArgs& p, float* to, size_
     for (int i = 0; i < SP; ++i)
         if (on && s0 + i < p.S) to[(row * p.D + ch) * p.S + s0 + i] = lane_of(h[i / 2], i & 1);
 }
-// B and C of steps t .. t + STEPS - 1 of sequence n as fp32, zero behind the last state and at steps from `end` on.
-template <typename T, int STEPS, int SP, int NT>
-__device__ __forceinline__ void stage_bc(const ScanArgs& p, const T* b, const T* c, int n, int t, int end, float (*sb)[SP], float (*sc)[SP])
+// Steps t .. t + ROWS - 1 of sequence n, channels c0 .. c0 + CB - 1, to shared memory; zeros behind the last step and channel.  WIDE: by
+// asynchronous copies of 16 bytes (rows and channels start on such boundaries), else element by element.
+template <typename T, bool WIDE, int ROWS, int CB>
+__device__ __forceinline__ void copy_rows(const ScanArgs& p, T (*to)[CB], const T* from, int64_t ld, int n, int t, int end, int c0)
 {
+    constexpr int PER = WIDE ? 16 / sizeof(T) : 1, PIECES = CB / PER;
 #pragma unroll
-    for (int e0 = 0; e0 < STEPS * SP; e0 += NT) {
-        const int e = e0 + threadIdx.x, j = e / SP, s = e % SP;
-        if (STEPS * SP % NT && e >= STEPS * SP) break;
-        const bool on = s < p.S && t + j < end;
-        const size_t row = (size_t)(t + j) * p.N + n;
-        sb[j][s] = on ? to_float(b[row * p.ld_b + s]) : 0.f;
-        sc[j][s] = on && c ? to_float(c[row * p.ld_c + s]) : 0.f;
+    for (int e0 = 0; e0 < ROWS * PIECES; e0 += kThreads) {
+        const int e = e0 + threadIdx.x, j = e / PIECES, c = e % PIECES * PER;
+        if (ROWS * PIECES % kThreads && e >= ROWS * PIECES) break;
+        const bool on = t + j < end && c0 + c < p.D;
+        const T* at = from + (on ? ((int64_t)(t + j) * p.N + n) * ld + c0 + c : 0);
+        if (WIDE) copy16(&to[j][c], at, on);
+        else to[j][c] = on ? *at : from_float<T>(0.f);
     }
 }
-
-// Pairs of a thread's states whose decays the multiply-adds compute.
-template <int SPT> constexpr int kScanPoly = SPT == 16 ? 3 : SPT == 8 ? 2 : 1;
-template <int SPT> constexpr int kGradientPoly = SPT == 8 ? 2 : 1;
 
 enum Mode { SCAN, MAPS, MAPS_BACK };            // outputs; the runs' maps; those and what the runs hand back
 
 // SPT states a thread, LS lanes a channel.  dy: MAPS_BACK only, in the place of y.
-template <typename T, int SPT, int LS, Mode MODE>
-__global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const T* x, const T* dt, const T* b, const T* c, const T* z, const T* dy, const float* first,
+template <typename T, int SPT, int LS, Mode MODE, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 5) scan_kernel(const ScanArgs p, const T* x, const T* dt, const T* b, const T* c, const T* z, const T* dy, const float* first,
                                                         T* y, float* state_out, RunMaps m)
 {
-    constexpr int SP = SPT * LS, CB = kThreads / LS, NP = kScanPoly<SPT>;
+    constexpr int SP = SPT * LS, CB = kThreads / LS;
+    constexpr int TILES = MODE == MAPS ? 2 : MODE == SCAN ? 3 : 4;
+    __shared__ __align__(16) T tile[kStages][TILES][kGroup][CB];                // x, dt, z, dy
     __shared__ __align__(16) float sb[2][kGroup][SP], sc[2][kGroup][SP];
-    __shared__ uint8_t fresh[2][kGroup];
+    static_assert(kGroup <= 8, "start_at");
     pdl_wait();
     pdl_trigger();
     const int across = (p.D + CB - 1) / CB;
@@ -179,12 +154,11 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const 
     const int sub = threadIdx.x % LS, own = (int)(blockIdx.x % across) * CB + threadIdx.x / LS, s0 = sub * SPT;
     const bool on = own < p.D;
     const int ch = on ? own : 0;
-    const int end = steps_of(p.lengths, n, p.T);
+    const int end = uniform(steps_of(p.lengths, n, p.T));
     const int t0 = min(run * p.length, end), t1 = min(t0 + p.length, end);
 
     f32x2 a2[SPT / 2], h[SPT / 2], prod[SPT / 2], back[SPT / 2];
     load_decays<SPT>(p, ch, s0, on, a2);
-    const float limit = small_delta<NP>(a2);
     load_states<SPT>(p, MODE == SCAN ? first : nullptr, (size_t)run * p.N + n, ch, s0, on, h);
     if (MODE == MAPS_BACK)
 #pragma unroll
@@ -193,68 +167,98 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs p, const 
     float sum = 0.f;
     bool broken = false;
 
-    for (int t = t0, buf = 0; t < t1; t += kGroup, buf ^= 1) {
-        stage_bc<T, kGroup, SP, kThreads>(p, b, MODE == MAPS ? nullptr : c, n, t, t1, sb[buf], sc[buf]);
-        if (threadIdx.x < kGroup) fresh[buf][threadIdx.x] = p.starts && t + (int)threadIdx.x < t1 ? p.starts[(size_t)(t + threadIdx.x) * p.N + n] : 0;
-        T rx[kGroup], rdt[kGroup], rz[kGroup], rg[kGroup];
+    // Groups of steps are on their way to shared memory kStages - 1 ahead; B, C and the starts in registers one ahead.
+    constexpr int BC = (kGroup * SP + kThreads - 1) / kThreads;
+    const int c0 = (int)(blockIdx.x % across) * CB, cl = threadIdx.x / LS;
+    T rb[BC], rc[BC];
+    uint8_t rst = 0;
+    auto ask = [&](int t) {
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
-            const size_t row = (size_t)min(t + j, t1 - 1) * p.N + n;
-            rx[j] = x[row * p.ld_x + ch];
-            rdt[j] = dt[row * p.ld_dt + ch];
-            if (MODE != MAPS && z) rz[j] = z[row * p.ld_z + ch];
-            if (MODE == MAPS_BACK) rg[j] = dy[row * p.ld_y + ch];
+        for (int i = 0; i < BC; ++i) {
+            const int e = threadIdx.x + i * kThreads, s = e % SP;
+            if (s < p.S && t + e / SP < t1) {
+                const int64_t row = (int64_t)(t + e / SP) * p.N + n;
+                rb[i] = b[row * p.ld_b + s];
+                if (MODE != MAPS) rc[i] = c[row * p.ld_c + s];
+            }
         }
-        __syncthreads();                        // the other buffer's readers have passed the barrier before
+        rst = start_at(p, n, t, t1);
+    };
+    auto send = [&](int t, int stage) {
+        if (t < t1) {
+            copy_rows<T, WIDE, kGroup, CB>(p, tile[stage][0], x, p.ld_x, n, t, t1, c0);
+            copy_rows<T, WIDE, kGroup, CB>(p, tile[stage][1], dt, p.ld_dt, n, t, t1, c0);
+            if (MODE != MAPS && z) copy_rows<T, WIDE, kGroup, CB>(p, tile[stage][2], z, p.ld_z, n, t, t1, c0);
+            if (MODE == MAPS_BACK) copy_rows<T, WIDE, kGroup, CB>(p, tile[stage][3], dy, p.ld_y, n, t, t1, c0);
+        }
+        copies_commit();
+    };
+    if (t0 < t1) ask(t0);
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
-            if (t + j >= t1) break;
-            const float xv = to_float(rx[j]), raw = to_float(rdt[j]) + bias, delta = p.softplus ? softplus(raw) : raw;
-            if (fresh[buf][j]) {
+    for (int i = 0; i < kStages - 1; ++i) send(t0 + i * kGroup, i);
+    int stage = 0;
+    for (int t = t0, buf = 0; t < t1; t += kGroup, buf ^= 1) {
 #pragma unroll
-                for (int i = 0; i < SPT / 2; ++i) h[i] = both(0.f);
-                broken = true;
-            }
-            sum += delta;
-            const f32x2 d2 = both(delta), u2 = both(delta * xv);
-            const bool small = fabsf(delta) < limit;
-            float g = 0.f;
-            if (MODE == MAPS_BACK) {
-                g = to_float(rg[j]);
-                if (z) g *= silu(to_float(rz[j]));
-            }
-            f32x2 acc[2] = {both(0.f), both(0.f)};
-            by_size<NP>(small, [&](auto poly) {
+        for (int i = 0; i < BC; ++i) {                                          // zero behind the last state and step
+            const int e = threadIdx.x + i * kThreads, j = e / SP, s = e % SP;
+            if (kGroup * SP % kThreads && e >= kGroup * SP) break;
+            const bool live = s < p.S && t + j < t1;
+            sb[buf][j][s] = live ? to_float(rb[i]) : 0.f;
+            if (MODE != MAPS) sc[buf][j][s] = live ? to_float(rc[i]) : 0.f;
+        }
+        const uint32_t fresh = __ballot_sync(0xffffffffu, rst != 0);
+        copies_wait<kStages - 2>();
+        __syncthreads();                        // the copies of all threads have landed; all have left the group before
+        send(t + (kStages - 1) * kGroup, stage == 0 ? kStages - 1 : stage - 1);
+        if (t + kGroup < t1) ask(t + kGroup);
+        // the steps, without a branch between them unless an episode begins in the group
+        auto steps = [&](auto with_starts) {
 #pragma unroll
-            for (int i = 0; i < SPT / 2; i += 2) {
-                const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[buf][j][s0 + 2 * i]);
-                const f32x2 bb[2] = {bv.x, bv.y};
-                f32x2 cc[2] = {0, 0};
-                if (MODE != MAPS) {
-                    const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[buf][j][s0 + 2 * i]);
-                    cc[0] = cv.x; cc[1] = cv.y;
+            for (int j = 0; j < kGroup; ++j) {
+                if (decltype(with_starts)::value && (fresh >> j & 1)) {
+#pragma unroll
+                    for (int i = 0; i < SPT / 2; ++i) h[i] = both(0.f);
+                    if (MODE == MAPS_BACK) broken = true;
                 }
+                const float xv = to_float(tile[stage][0][j][cl]), raw = to_float(tile[stage][1][j][cl]) + bias, full = p.softplus ? softplus(raw) : raw;
+                const float delta = t + j < t1 ? full : 0.f;                    // steps behind the run's end: nothing in, all kept
+                float gate = MODE != MAPS && z ? silu(to_float(tile[stage][TILES > 2 ? 2 : 0][j][cl])) : 1.f;
+                if (MODE == MAPS_BACK) gate *= to_float(tile[stage][TILES > 3 ? 3 : 0][j][cl]);
+                sum += delta;
+                const f32x2 d2 = both(delta), u2 = both(delta * xv);
+                f32x2 acc[2] = {both(0.f), both(0.f)};
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const f32x2 decay = exp2_pair<decltype(poly)::value>(mul2(d2, a2[i + k]), i + k);
-                    h[i + k] = fma2(decay, h[i + k], mul2(u2, bb[k]));
-                    if (MODE == SCAN) acc[k] = fma2(cc[k], h[i + k], acc[k]);
-                    if (MODE == MAPS_BACK && !broken) {
-                        prod[i + k] = mul2(prod[i + k], decay);
-                        back[i + k] = fma2(mul2(both(g), cc[k]), prod[i + k], back[i + k]);
+                for (int i = 0; i < SPT / 2; i += 2) {
+                    const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[buf][j][s0 + 2 * i]);
+                    const f32x2 bb[2] = {bv.x, bv.y};
+                    f32x2 cc[2] = {0, 0};
+                    if (MODE != MAPS) {
+                        const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[buf][j][s0 + 2 * i]);
+                        cc[0] = cv.x; cc[1] = cv.y;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const f32x2 decay = decay_pair(d2, a2[i + k]);
+                        h[i + k] = fma2(decay, h[i + k], mul2(u2, bb[k]));
+                        if (MODE == SCAN) acc[k] = fma2(cc[k], h[i + k], acc[k]);
+                        if (MODE == MAPS_BACK && !broken) {
+                            prod[i + k] = mul2(prod[i + k], decay);
+                            back[i + k] = fma2(mul2(both(gate), cc[k]), prod[i + k], back[i + k]);
+                        }
                     }
                 }
-            }
-            });
-            if (MODE == SCAN) {
-                float v = (lane_of(acc[0], 0) + lane_of(acc[1], 0)) + (lane_of(acc[0], 1) + lane_of(acc[1], 1));
+                if (MODE == SCAN) {
+                    float v = (lane_of(acc[0], 0) + lane_of(acc[1], 0)) + (lane_of(acc[0], 1) + lane_of(acc[1], 1));
 #pragma unroll
-                for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                v = fmaf(skip, xv, v);
-                if (z) v *= silu(to_float(rz[j]));
-                if (on && sub == 0) y[((size_t)(t + j) * p.N + n) * p.ld_y + ch] = from_float<T>(v);
+                    for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                    if (on && sub == 0 && t + j < t1) (y + ((int64_t)(t + j) * p.N + n) * p.ld_y)[ch] = from_float<T>(fmaf(skip, xv, v) * gate);
+                }
             }
-        }
+        };
+        if (fresh) steps(std::true_type());
+        else steps(std::false_type());
+        broken = broken || fresh;
+        if (++stage == kStages) stage = 0;
     }
     if (MODE == SCAN) {
         if (state_out && run == p.runs - 1) store_states<SPT>(p, state_out, n, ch, s0, on, h);
@@ -393,18 +397,19 @@ constexpr int kChunk = 8;
 // of the state walks back over them.  Sums over channels (dB, dC) are taken from shared memory too: a thread takes four
 // states of a step and adds the products of a share of the block's channels, which costs one load and two packed
 // multiply-adds for four terms, where exchanges between lanes would take two of each for every term.
-template <typename T, int SPT, int LS>
-__global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs p, const GradArgs q, const T* x, const T* dt, const T* b, const T* c, const T* z,
+template <typename T, int SPT, int LS, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 4) scan_gradient_kernel(const ScanArgs p, const GradArgs q, const T* x, const T* dt, const T* b, const T* c, const T* z,
                                                                  const T* dy, T* dx, T* ddt, T* dz)
 {
-    constexpr int SP = SPT * LS, CB = kThreads / LS, Q = SPT / 4, ITEMS = kChunk * CB / kThreads, NP = kGradientPoly<SPT>;
+    constexpr int SP = SPT * LS, CB = kThreads / LS, Q = SPT / 4, ITEMS = kChunk * CB / kThreads;
     extern __shared__ __align__(16) float s_mem[];
     float4* hs = reinterpret_cast<float4*>(s_mem);                              // [kChunk][Q][kThreads]: states, then their gradients
     float* s_delta = s_mem + kChunk * SPT * kThreads;                           // [kChunk][CB] each
     float *s_x = s_delta + kChunk * CB, *s_g = s_x + kChunk * CB, *s_gb = s_g + kChunk * CB, *s_gk = s_gb + kChunk * CB, *s_y = s_gk + kChunk * CB;
     float(*sb)[SP] = reinterpret_cast<float(*)[SP]>(s_y + kChunk * CB);
     float(*sc)[SP] = sb + kChunk;
-    uint8_t* fresh = reinterpret_cast<uint8_t*>(sc + kChunk);
+    T(*tile)[4][kChunk][CB] = reinterpret_cast<T(*)[4][kChunk][CB]>(sc + kChunk);      // [2]: x, dt, z, dy
+    static_assert(kChunk <= 8, "start_at");
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, across = (p.D + CB - 1) / CB, cb = (int)(blockIdx.x % across);
@@ -412,7 +417,7 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
     const int sub = tid % LS, cl = tid / LS, s0 = sub * SPT, own = cb * CB + cl;
     const bool on = own < p.D;
     const int ch = on ? own : 0, channels = min(CB, p.D - cb * CB);
-    const int end = steps_of(p.lengths, n, p.T);
+    const int end = uniform(steps_of(p.lengths, n, p.T));
     const int t0 = min(run * p.length, end), t1 = min(t0 + p.length, end), chunks = (t1 - t0 + kChunk - 1) / kChunk;
     // the channel whose inputs and outputs this thread converts: the same for all its items
     const int ic = tid % CB, ich = min(cb * CB + ic, p.D - 1);
@@ -422,7 +427,6 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
 
     f32x2 a2[SPT / 2], h[SPT / 2], carry[SPT / 2], da[SPT / 2];
     load_decays<SPT>(p, ch, s0, on, a2);
-    const float limit = small_delta<NP>(a2);
     load_states<SPT>(p, q.first, row0, ch, s0, on, h);
     load_states<SPT>(p, q.incoming, row0, ch, s0, on, carry);
 #pragma unroll
@@ -430,44 +434,48 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
     float dskip = 0.f, dbias = 0.f;
     float4* checks = reinterpret_cast<float4*>(q.checks) + (size_t)blockIdx.x * q.chunks * Q * kThreads + tid;
 
-    auto advance = [&](int j, f32x2 (&h)[SPT / 2]) {                            // one step of the state
+    uint32_t fresh = 0;                                                         // the chunk's steps that begin an episode
+    auto advance = [&](auto with_starts, int j, f32x2 (&h)[SPT / 2]) {          // one step of the state
         const int at = j * CB + cl;
         const float delta = s_delta[at];
         const f32x2 d2 = both(delta), u2 = both(delta * s_x[at]);
-        if (fresh[j])
+        if (decltype(with_starts)::value && (fresh >> j & 1))
 #pragma unroll
             for (int i = 0; i < SPT / 2; ++i) h[i] = both(0.f);
-        by_size<NP>(fabsf(delta) < limit, [&](auto poly) {
 #pragma unroll
-            for (int i = 0; i < SPT / 2; i += 2) {
-                const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 2 * i]);
-                h[i] = fma2(exp2_pair<decltype(poly)::value>(mul2(d2, a2[i]), i), h[i], mul2(u2, bv.x));
-                h[i + 1] = fma2(exp2_pair<decltype(poly)::value>(mul2(d2, a2[i + 1]), i + 1), h[i + 1], mul2(u2, bv.y));
-            }
-        });
-    };
-    // A chunk's inputs as they lie in memory: asked for while the chunk before is worked on.
-    constexpr int BC = (kChunk * SP + kThreads - 1) / kThreads;
-    T rx[ITEMS], rdt[ITEMS], rg[ITEMS], rz[ITEMS], rb[BC], rc[BC];
-    uint8_t rst = 0;
-    const int first_row = tid / CB, rows_apart = kThreads / CB;
-    auto ask = [&](int t, bool all) {
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const size_t row = (size_t)min(t + first_row + i * rows_apart, t1 - 1) * p.N + n;
-            rdt[i] = dt[row * p.ld_dt + ich];
-            rx[i] = x[row * p.ld_x + ich];
-            if (all) rg[i] = dy[row * q.ld_dy + ich];
-            if (all && z) rz[i] = z[row * p.ld_z + ich];
+        for (int i = 0; i < SPT / 2; i += 2) {
+            const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 2 * i]);
+            h[i] = fma2(decay_pair(d2, a2[i]), h[i], mul2(u2, bv.x));
+            h[i + 1] = fma2(decay_pair(d2, a2[i + 1]), h[i + 1], mul2(u2, bv.y));
         }
+    };
+    auto by_starts = [&](auto f) {                                              // a chunk without one has no branch between its steps
+        if (fresh) f(std::true_type());
+        else f(std::false_type());
+    };
+    // A chunk's inputs are on their way to shared memory, B, C and the starts to registers, while the chunk before is worked on.
+    constexpr int BC = (kChunk * SP + kThreads - 1) / kThreads;
+    T rb[BC], rc[BC];
+    uint8_t rst = 0;
+    const int first_row = tid / CB;
+    constexpr int APART = kThreads / CB;
+    const int64_t my_row = (int64_t)first_row * p.N;
+    auto ask = [&](int t, int slot, bool all) {
+        copy_rows<T, WIDE, kChunk, CB>(p, tile[slot][0], x, p.ld_x, n, t, t1, cb * CB);
+        copy_rows<T, WIDE, kChunk, CB>(p, tile[slot][1], dt, p.ld_dt, n, t, t1, cb * CB);
+        if (all && z) copy_rows<T, WIDE, kChunk, CB>(p, tile[slot][2], z, p.ld_z, n, t, t1, cb * CB);
+        if (all) copy_rows<T, WIDE, kChunk, CB>(p, tile[slot][3], dy, q.ld_dy, n, t, t1, cb * CB);
+        copies_commit();
 #pragma unroll
         for (int i = 0; i < BC; ++i) {
-            const int e = tid + i * kThreads, s = min(e % SP, p.S - 1);
-            const size_t row = (size_t)min(t + e / SP, t1 - 1) * p.N + n;
-            rb[i] = b[row * p.ld_b + s];
-            if (all) rc[i] = c[row * p.ld_c + s];
+            const int e = tid + i * kThreads, s = e % SP;
+            if (s < p.S && t + e / SP < t1) {
+                const int64_t row = (int64_t)(t + e / SP) * p.N + n;
+                rb[i] = b[row * p.ld_b + s];
+                if (all) rc[i] = c[row * p.ld_c + s];
+            }
         }
-        if (tid < kChunk) rst = p.starts ? p.starts[(size_t)min(t + tid, t1 - 1) * p.N + n] : 0;
+        rst = start_at(p, n, t, t1);
     };
     auto stage_bc_starts = [&](int t, bool all) {                               // zero behind the last state and step
 #pragma unroll
@@ -478,38 +486,42 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
             sb[j][s] = live ? to_float(rb[i]) : 0.f;
             if (all) sc[j][s] = live ? to_float(rc[i]) : 0.f;
         }
-        if (tid < kChunk) fresh[tid] = t + tid < t1 ? rst : 0;
+        fresh = __ballot_sync(0xffffffffu, rst != 0);
     };
 
-    if (chunks > 1) ask(t0, false);
+    if (chunks) ask(t0, 0, chunks == 1);
     for (int k = 0; k < chunks; ++k) {                                          // states at the chunks' first steps
 #pragma unroll
         for (int i = 0; i < Q; ++i)
             checks[(size_t)(k * Q + i) * kThreads] = make_float4(lane_of(h[2 * i], 0), lane_of(h[2 * i], 1), lane_of(h[2 * i + 1], 0), lane_of(h[2 * i + 1], 1));
         if (k == chunks - 1) break;                                             // that one's steps come next
         const int t = t0 + k * kChunk;
+        copies_wait<0>();
         stage_bc_starts(t, false);
+        __syncthreads();                                                        // everybody's copies
+        ask(t + kChunk, (k + 1) & 1, k + 2 == chunks);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int e = tid + i * kThreads;
-            const float raw = to_float(rdt[i]) + ibias;
+            const float raw = to_float(tile[k & 1][1][e / CB][ic]) + ibias;
             s_delta[e] = ion ? (p.softplus ? softplus(raw) : raw) : 0.f;
-            s_x[e] = ion ? to_float(rx[i]) : 0.f;
+            s_x[e] = ion ? to_float(tile[k & 1][0][e / CB][ic]) : 0.f;
         }
         __syncthreads();
-        ask(t + kChunk, k + 2 >= chunks);
+        by_starts([&](auto with_starts) {
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) advance(j, h);
+            for (int j = 0; j < kChunk; ++j) advance(with_starts, j, h);
+        });
         __syncthreads();
     }
-    if (chunks == 1) ask(t0, true);
-
     f32x2 ahead[SPT / 2];                                                       // the next chunk's first state
 #pragma unroll
     for (int i = 0; i < SPT / 2; ++i) ahead[i] = h[i];
     for (int k = chunks - 1; k >= 0; --k) {
         const int t = t0 + k * kChunk;
+        copies_wait<0>();
         stage_bc_starts(t, true);
+        __syncthreads();                                                        // everybody's copies
         float slope_dt[ITEMS], slope_z[ITEMS];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {                                       // steps behind the end: nothing in, all kept
@@ -518,12 +530,12 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
             float delta = 0.f, xv = 0.f, g = 0.f;
             slope_dt[i] = 1.f; slope_z[i] = 0.f;
             if (live) {
-                const float raw = to_float(rdt[i]) + ibias;
+                const float raw = to_float(tile[k & 1][1][e / CB][ic]) + ibias;
                 delta = p.softplus ? softplus(raw, &slope_dt[i]) : raw;
-                xv = to_float(rx[i]);
-                g = to_float(rg[i]);
+                xv = to_float(tile[k & 1][0][e / CB][ic]);
+                g = to_float(tile[k & 1][3][e / CB][ic]);
                 if (z) {
-                    const float zv = to_float(rz[i]), sg = sigmoid(zv);
+                    const float zv = to_float(tile[k & 1][2][e / CB][ic]), sg = sigmoid(zv);
                     slope_z[i] = g * (sg * (1.f + zv * (1.f - sg)));
                     g *= zv * sg;
                 }
@@ -536,7 +548,7 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
         for (int i = 0; i < SPT / 2; ++i) h[i] = h0[i] = ahead[i];
         __syncthreads();
         if (k) {
-            ask(t - kChunk, true);
+            ask(t - kChunk, (k - 1) & 1, true);
 #pragma unroll
             for (int i = 0; i < Q; ++i) {
                 const float4 v = checks[(size_t)((k - 1) * Q + i) * kThreads];
@@ -544,22 +556,24 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
                 ahead[2 * i + 1] = pair(v.z, v.w);
             }
         }
-#pragma unroll 2
-        for (int j = 0; j < kChunk; ++j) {                                      // the chunk's states, and the sums over them
-            advance(j, h);
-            f32x2 acc = both(0.f);
+        by_starts([&](auto with_starts) {
 #pragma unroll
-            for (int i = 0; i < Q; ++i) {
-                const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]);
-                acc = fma2(cv.x, h[2 * i], acc);
-                acc = fma2(cv.y, h[2 * i + 1], acc);
-                *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(h[2 * i], h[2 * i + 1]);
+            for (int j = 0; j < kChunk; ++j) {                                  // the chunk's states, and the sums over them
+                advance(with_starts, j, h);
+                f32x2 acc = both(0.f);
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]);
+                    acc = fma2(cv.x, h[2 * i], acc);
+                    acc = fma2(cv.y, h[2 * i + 1], acc);
+                    *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(h[2 * i], h[2 * i + 1]);
+                }
+                float v = lane_of(acc, 0) + lane_of(acc, 1);
+#pragma unroll
+                for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                if (sub == 0) s_y[j * CB + cl] = v;
             }
-            float v = lane_of(acc, 0) + lane_of(acc, 1);
-#pragma unroll
-            for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-            if (sub == 0) s_y[j * CB + cl] = v;
-        }
+        });
         __syncthreads();
         // sums over the block's channels of weight x what hs holds, four states of a step to a thread and a share of the channels
         auto over_channels = [&](auto weight, int half) {
@@ -587,53 +601,53 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
         };
         over_channels([&](int at) { return s_g[at]; }, 1);
         __syncthreads();
-#pragma unroll 2
-        for (int j = kChunk - 1; j >= 0; --j) {                                 // back over the chunk
-            const int at = j * CB + cl;
-            const float delta = s_delta[at];
-            const f32x2 d2 = both(delta), g2 = both(s_g[at]);
-            const bool st = fresh[j], small = fabsf(delta) < limit;
-            f32x2 gb = both(0.f), gk = both(0.f);
-            by_size<NP>(small, [&](auto poly) {
+        by_starts([&](auto with_starts) {
 #pragma unroll
-            for (int i = 0; i < Q; ++i) {
-                const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]), bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 4 * i]);
-                ulonglong2 old = j ? *reinterpret_cast<const ulonglong2*>(&hs[((j - 1) * Q + i) * kThreads + tid]) : make_ulonglong2(h0[2 * i], h0[2 * i + 1]);
-                if (st) old = make_ulonglong2(0, 0);
-                const f32x2 c2[2] = {cv.x, cv.y}, b2[2] = {bv.x, bv.y}, o2[2] = {old.x, old.y};
-                f32x2 grad[2];
+            for (int j = kChunk - 1; j >= 0; --j) {                             // back over the chunk
+                const int at = j * CB + cl;
+                const float delta = s_delta[at];
+                const f32x2 d2 = both(delta), g2 = both(s_g[at]);
+                const bool st = decltype(with_starts)::value && (fresh >> j & 1);
+                f32x2 gb = both(0.f), gk = both(0.f);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int w = 2 * i + e;
-                    const f32x2 decay = exp2_pair<decltype(poly)::value>(mul2(d2, a2[w]), w);
-                    grad[e] = fma2(g2, c2[e], carry[w]);
-                    const f32x2 kept = mul2(grad[e], mul2(decay, o2[e]));
-                    gk = fma2(a2[w], kept, gk);
-                    da[w] = fma2(d2, kept, da[w]);
-                    gb = fma2(grad[e], b2[e], gb);
-                    carry[w] = st ? both(0.f) : mul2(decay, grad[e]);
+                for (int i = 0; i < Q; ++i) {
+                    const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]), bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 4 * i]);
+                    ulonglong2 old = j ? *reinterpret_cast<const ulonglong2*>(&hs[((j - 1) * Q + i) * kThreads + tid]) : make_ulonglong2(h0[2 * i], h0[2 * i + 1]);
+                    if (st) old = make_ulonglong2(0, 0);
+                    const f32x2 c2[2] = {cv.x, cv.y}, b2[2] = {bv.x, bv.y}, o2[2] = {old.x, old.y};
+                    f32x2 grad[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int w = 2 * i + e;
+                        const f32x2 decay = decay_pair(d2, a2[w]);
+                        grad[e] = fma2(g2, c2[e], carry[w]);
+                        const f32x2 flow = mul2(decay, grad[e]), kept = mul2(flow, o2[e]);
+                        gk = fma2(a2[w], kept, gk);
+                        da[w] = fma2(d2, kept, da[w]);
+                        gb = fma2(grad[e], b2[e], gb);
+                        carry[w] = st ? both(0.f) : flow;
+                    }
+                    *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(grad[0], grad[1]);
                 }
-                *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(grad[0], grad[1]);
-            }
-            });
-            float vb = lane_of(gb, 0) + lane_of(gb, 1), vk = lane_of(gk, 0) + lane_of(gk, 1);
+                float vb = lane_of(gb, 0) + lane_of(gb, 1), vk = lane_of(gk, 0) + lane_of(gk, 1);
 #pragma unroll
-            for (int o = 1; o < LS; o <<= 1) { vb += __shfl_xor_sync(0xffffffffu, vb, o); vk += __shfl_xor_sync(0xffffffffu, vk, o); }
-            if (sub == 0) { s_gb[at] = vb; s_gk[at] = vk; }
-        }
+                for (int o = 1; o < LS; o <<= 1) { vb += __shfl_xor_sync(0xffffffffu, vb, o); vk += __shfl_xor_sync(0xffffffffu, vk, o); }
+                if (sub == 0) { s_gb[at] = vb; s_gk[at] = vk; }
+            }
+        });
         __syncthreads();
         over_channels([&](int at) { return s_delta[at] * s_x[at]; }, 0);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int e = tid + i * kThreads;
             if (ion && t + e / CB < t1) {
-                const size_t row = (size_t)(t + e / CB) * p.N + n;
+                const int64_t row = (int64_t)(t + i * APART) * p.N + n;
                 const float xv = s_x[e], gb = s_gb[e];
                 const float dd = fmaf(xv, gb, s_gk[e] * (1.f / kLog2e)) * slope_dt[i];       // a2 is A log2(e)
                 dbias += dd;
-                if (dx) dx[row * q.ld_dx + ich] = from_float<T>(fmaf(s_delta[e], gb, iskip * s_g[e]));
-                if (ddt) ddt[row * q.ld_ddt + ich] = from_float<T>(dd);
-                if (dz) dz[row * q.ld_dz + ich] = from_float<T>(slope_z[i] * fmaf(iskip, xv, s_y[e]));
+                if (dx) (dx + my_row * q.ld_dx + ich)[row * q.ld_dx] = from_float<T>(fmaf(s_delta[e], gb, iskip * s_g[e]));
+                if (ddt) (ddt + my_row * q.ld_ddt + ich)[row * q.ld_ddt] = from_float<T>(dd);
+                if (dz) (dz + my_row * q.ld_dz + ich)[row * q.ld_dz] = from_float<T>(slope_z[i] * fmaf(iskip, xv, s_y[e]));
             }
         }
         __syncthreads();
@@ -654,9 +668,9 @@ __global__ void __launch_bounds__(kThreads) scan_gradient_kernel(const ScanArgs 
         }
     }
 }
-template <int SPT, int LS> constexpr size_t gradient_shared()
+template <typename T, int SPT, int LS> constexpr size_t gradient_shared()
 {
-    return (size_t)(kChunk * SPT * kThreads + 6 * kChunk * (kThreads / LS) + 2 * kChunk * SPT * LS) * 4 + 16;
+    return (size_t)(kChunk * SPT * kThreads + 6 * kChunk * (kThreads / LS) + 2 * kChunk * SPT * LS) * 4 + 8 * kChunk * (kThreads / LS) * sizeof(T);
 }
 
 // dB and dC: the channel blocks' parts added in order.
@@ -773,6 +787,15 @@ hts_status launch_compose(const ScanArgs& p, const float* state_in, const float*
     return HTS_OK;
 }
 
+// Whether the rows of every tensor, and the channels of every block, start on 16-byte boundaries.
+bool rows_of_16(int64_t D, size_t element, std::initializer_list<const void*> pointers, std::initializer_list<int64_t> strides)
+{
+    bool ok = D * element % 16 == 0;
+    for (const void* q : pointers) ok = ok && aligned_to(q, 16);
+    for (int64_t l : strides) ok = ok && l * element % 16 == 0;
+    return ok;
+}
+
 template <typename T>
 hts_status forward(ScanArgs p, const hts_scan_inputs& in, T* y, float* state_out, void* workspace, cudaStream_t s)
 {
@@ -780,20 +803,21 @@ hts_status forward(ScanArgs p, const hts_scan_inputs& in, T* y, float* state_out
     p.runs = q.runs; p.length = q.length;
     const T *x = (const T*)in.x, *dt = (const T*)in.dt, *b = (const T*)in.b, *c = (const T*)in.c, *z = (const T*)in.z, *none = nullptr;
     const unsigned row = (unsigned)(q.across * p.N);
+    const bool wide = rows_of_16(p.D, sizeof(T), {x, dt, z}, {p.ld_x, p.ld_dt, z ? p.ld_z : 0});
     return by_scan_shape(p.S, [&](auto spt, auto ls) {
         constexpr int SPT = decltype(spt)::value, LS = decltype(ls)::value;
         const float* first = in.state_in;
         RunMaps m{};
         if (q.runs > 1) {
             m = maps_at(q, workspace);
-            HTS_CUDA(launch_pdl(scan_kernel<T, SPT, LS, MAPS>, dim3(row * (q.runs - 1)), dim3(kThreads), 0, s, p, x, dt, b, c, z, none, (const float*)nullptr, (T*)nullptr,
+            HTS_CUDA(launch_pdl(wide ? scan_kernel<T, SPT, LS, MAPS, true> : scan_kernel<T, SPT, LS, MAPS, false>, dim3(row * (q.runs - 1)), dim3(kThreads), 0, s, p, x, dt, b, c, z, none, (const float*)nullptr, (T*)nullptr,
                                 (float*)nullptr, m));
             note_launch();
             const hts_status st = launch_compose(p, in.state_in, nullptr, m, false, s);
             if (st != HTS_OK) return st;
             first = m.ends;
         }
-        HTS_CUDA(launch_pdl(scan_kernel<T, SPT, LS, SCAN>, dim3(row * q.runs), dim3(kThreads), 0, s, p, x, dt, b, c, z, none, first, y, state_out, m));
+        HTS_CUDA(launch_pdl(wide ? scan_kernel<T, SPT, LS, SCAN, true> : scan_kernel<T, SPT, LS, SCAN, false>, dim3(row * q.runs), dim3(kThreads), 0, s, p, x, dt, b, c, z, none, first, y, state_out, m));
         note_launch();
         return HTS_OK;
     });
@@ -832,7 +856,7 @@ hts_status gradient(ScanArgs p, const hts_scan_inputs& in, const T* dy, int64_t 
     const T *x = (const T*)in.x, *dt = (const T*)in.dt, *b = (const T*)in.b, *c = (const T*)in.c, *z = (const T*)in.z;
     const unsigned row = (unsigned)(q.across * p.N);
     char* w = (char*)workspace;
-    const bool sums = out.a || out.d || out.dt_bias;
+    const bool sums = out.a || out.d || out.dt_bias, wide = rows_of_16(p.D, sizeof(T), {x, dt, z, dy}, {p.ld_x, p.ld_dt, z ? p.ld_z : 0, ld_dy});
     GradArgs g{ld_dy, out.ld_x, out.ld_dt, out.ld_z, (float*)(w + q.checks), (float*)(w + q.part_bc), sums ? (float*)(w + q.part_ch) : nullptr, in.state_in, dstate_out,
                out.state_in, q.chunks};
     if (q.runs > 1) {
@@ -842,7 +866,7 @@ hts_status gradient(ScanArgs p, const hts_scan_inputs& in, const T* dy, int64_t 
         const hts_status st = by_scan_shape(p.S, [&](auto spt, auto ls) {
             constexpr int SPT = decltype(spt)::value, LS = decltype(ls)::value;
             const unsigned blocks = (unsigned)(channel_blocks(p.D, {SPT, LS}) * p.N * q.runs);
-            HTS_CUDA(launch_pdl(scan_kernel<T, SPT, LS, MAPS_BACK>, dim3(blocks), dim3(kThreads), 0, s, e, x, dt, b, c, z, dy, (const float*)nullptr, (T*)nullptr,
+            HTS_CUDA(launch_pdl(wide ? scan_kernel<T, SPT, LS, MAPS_BACK, true> : scan_kernel<T, SPT, LS, MAPS_BACK, false>, dim3(blocks), dim3(kThreads), 0, s, e, x, dt, b, c, z, dy, (const float*)nullptr, (T*)nullptr,
                                 (float*)nullptr, m));
             note_launch();
             return launch_compose(p, in.state_in, dstate_out, m, true, s);
@@ -853,10 +877,10 @@ hts_status gradient(ScanArgs p, const hts_scan_inputs& in, const T* dy, int64_t 
     }
     hts_status st = by_gradient_shape(p.S, [&](auto spt, auto ls) {
         constexpr int SPT = decltype(spt)::value, LS = decltype(ls)::value;
-        static OncePerDevice allowed;
-        HTS_CUDA(allow_shared(scan_gradient_kernel<T, SPT, LS>, allowed));
-        HTS_CUDA(launch_pdl(scan_gradient_kernel<T, SPT, LS>, dim3(row * q.runs), dim3(kThreads), gradient_shared<SPT, LS>(), s, p, g, x, dt, b, c, z, dy, (T*)out.x,
-                            (T*)out.dt, (T*)out.z));
+        static OncePerDevice allowed[2];
+        auto kernel = wide ? scan_gradient_kernel<T, SPT, LS, true> : scan_gradient_kernel<T, SPT, LS, false>;
+        HTS_CUDA(allow_shared(kernel, allowed[wide]));
+        HTS_CUDA(launch_pdl(kernel, dim3(row * q.runs), dim3(kThreads), gradient_shared<T, SPT, LS>(), s, p, g, x, dt, b, c, z, dy, (T*)out.x, (T*)out.dt, (T*)out.z));
         note_launch();
         return HTS_OK;
     });
