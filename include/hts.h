@@ -480,6 +480,33 @@ hts_status hts_selective_scan_gradient(const hts_scan_desc *desc, const hts_scan
                                        const float *dstate_out_or_null, const hts_scan_grads *grads, void *workspace,
                                        int64_t workspace_bytes, void *cuda_stream);
 
+typedef struct {
+    int32_t rows, in_features, out_features;
+    int32_t activation;         /* HTS_ACT_*                                        */
+    int64_t ld_x, ld_residual, ld_y, ld_pre;
+    int64_t ld_dy, ld_dx;       /* read by hts_linear_gradient only                 */
+    int32_t dw_dtype;           /* of dw: HTS_DTYPE_*, read by hts_linear_gradient only */
+} hts_linear_desc;
+
+/* A dense layer with its epilogue:  pre = x w^T + bias,  y = act(pre) + residual.
+ *   x rows of in_features; residual_or_null, y, pre_or_null (out) rows of out_features: bf16, [rows] of them
+ *   w DEVICE bf16 [out_features,in_features];  bias_or_null DEVICE f32 [out_features]
+ * Sums in fp32 on the tensor cores; pre and y are rounded once, y not by way of pre.  Any sizes; rows and weights
+ * that do not start on 16-byte boundaries are copied into the workspace first.
+ * y may be the residual itself.  Errors: INVALID_ARG, CUDA.                              */
+int64_t hts_linear_workspace(int32_t rows, int32_t in_features, int32_t out_features, int32_t gradient);
+hts_status hts_linear(const hts_linear_desc *desc, const void *x, const void *w, const float *bias_or_null,
+                      const void *residual_or_null, void *y, void *pre_or_null, void *workspace, int64_t workspace_bytes,
+                      void *cuda_stream);
+
+/* Its gradients, given dy:  dz = dy act'(pre), dx = dz w, dw = dz^T x, dbias = sum of dz; the residual's is dy.
+ *   pre rows bf16, as hts_linear left them (not read for HTS_ACT_NONE);  dx rows bf16;  dw [out_features,in_features];
+ *   dbias f32: each may be NULL, not all.
+ * With an activation dz is rounded to bf16 for the products (dbias adds it unrounded); sums in fp32, in a fixed order.  */
+hts_status hts_linear_gradient(const hts_linear_desc *desc, const void *x, const void *w, const void *pre_or_null,
+                               const void *dy, void *dx, void *dw, float *dbias, void *workspace, int64_t workspace_bytes,
+                               void *cuda_stream);
+
 /* Number of kernel launches this library has enqueued since it was loaded
  * (all contexts, all streams); for launch accounting by a benchmark.              */
 uint64_t hts_launch_count(void);

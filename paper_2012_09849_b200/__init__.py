@@ -30,7 +30,7 @@ EXPORTS = ("hts_policy_create", "hts_policy_load_weights", "hts_policy_step", "h
            "hts_policy_kernel_name", "hts_last_async_error", "hts_policy_destroy", "hts_gae",
            "hts_gae_host", "hts_gae_host_release", "hts_vtrace", "hts_causal_conv", "hts_causal_conv_step", "hts_causal_conv_gradient",
            "hts_causal_conv_workspace", "hts_selective_scan", "hts_selective_scan_step", "hts_selective_scan_gradient",
-           "hts_selective_scan_workspace", "hts_policy_step_noalloc", "hts_wait_selftest", "hts_launch_count", "hts_last_cuda_error", "hts_status_string")
+           "hts_selective_scan_workspace", "hts_linear", "hts_linear_gradient", "hts_linear_workspace", "hts_policy_step_noalloc", "hts_wait_selftest", "hts_launch_count", "hts_last_cuda_error", "hts_status_string")
 
 
 class HtsError(RuntimeError):
@@ -71,6 +71,11 @@ class hts_scan_inputs(C.Structure):
 class hts_scan_grads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("x", "dt", "b", "c", "z", "a", "d", "dt_bias", "state_in")] + \
                [(n, C.c_int64) for n in ("ld_x", "ld_dt", "ld_b", "ld_c", "ld_z")]
+
+
+class hts_linear_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "in_features", "out_features", "activation")] + \
+               [(n, C.c_int64) for n in ("ld_x", "ld_residual", "ld_y", "ld_pre", "ld_dy", "ld_dx")] + [("dw_dtype", C.c_int32)]
 
 
 _lib = None
@@ -143,6 +148,12 @@ def lib():
         L.hts_causal_conv_workspace.restype = C.c_int64
         L.hts_selective_scan_workspace.argtypes = [i32] * 5
         L.hts_selective_scan_workspace.restype = C.c_int64
+        L.hts_linear.argtypes = [C.POINTER(hts_linear_desc)] + [vp] * 7 + [C.c_int64, vp]
+        L.hts_linear.restype = C.c_int
+        L.hts_linear_gradient.argtypes = [C.POINTER(hts_linear_desc)] + [vp] * 8 + [C.c_int64, vp]
+        L.hts_linear_gradient.restype = C.c_int
+        L.hts_linear_workspace.argtypes = [i32] * 4
+        L.hts_linear_workspace.restype = C.c_int64
         L.hts_launch_count.restype = C.c_uint64
         L.hts_last_cuda_error.restype = C.c_char_p
         L.hts_status_string.restype = C.c_char_p
@@ -341,6 +352,21 @@ def hts_selective_scan_gradient(x, dt, a, b, c, d, dt_bias, z, starts, lengths, 
 def hts_selective_scan_workspace(T, N, channels, state, gradient=False) -> int:
     """Bytes of the workspace of hts_selective_scan, or of its gradient."""
     return lib().hts_selective_scan_workspace(int(T), int(N), int(channels), int(state), int(bool(gradient)))
+
+
+def hts_linear(x, w, bias, residual, activation, y, pre, workspace, stream=None) -> None:
+    """x [rows, in_features], y, pre, residual [rows, out_features]; activation: a key of ACTIVATIONS."""
+    _native.linear(x, w, bias, residual, ACTIVATIONS[activation], y, pre, workspace, stream)
+
+
+def hts_linear_gradient(x, w, pre, dy, activation, dx, dw, dbias, workspace, stream=None) -> None:
+    """dw: bfloat16 or float32."""
+    _native.linear_gradient(x, w, pre, dy, ACTIVATIONS[activation], dx, dw, dbias, workspace, stream)
+
+
+def hts_linear_workspace(rows, in_features, out_features, gradient=False) -> int:
+    """Bytes of the workspace of hts_linear, or of its gradient."""
+    return lib().hts_linear_workspace(int(rows), int(in_features), int(out_features), int(bool(gradient)))
 
 
 def hts_gae_host_release() -> None:

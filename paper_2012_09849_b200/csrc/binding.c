@@ -482,6 +482,59 @@ FN(selective_scan) { (void)self; return scan_like(a, nargs, 0); }
 FN(selective_scan_step) { (void)self; return scan_like(a, nargs, 1); }
 FN(selective_scan_gradient) { (void)self; return scan_like(a, nargs, 2); }
 
+FN(linear)
+{
+    (void)self;
+    ARGS(9);
+    int32_t dtype;
+    int64_t T, M, K, N, bytes;
+    hts_linear_desc d = {0};
+    void *x, *w, *res, *y, *pre, *work;
+    float *bias;
+    if (!to_lead(a[0], "x", 1, &dtype, &T, &M, &K) || !to_size(a[1], "w", BF16_T, 2, 0, &N)) return NULL;
+    dtype = BF16_T;
+    ROWS(a[0], "x", M, 0, K, x, d.ld_x);
+    DENSE(a[1], "w", BF16_T, N, K, 0, w);
+    DENSE(a[2], "bias", F32_T, N, 0, 0, bias);
+    ROWS(a[3], "residual", M, 0, N, res, d.ld_residual);
+    I32(act, 4);
+    ROWS(a[5], "y", M, 0, N, y, d.ld_y);
+    ROWS(a[6], "pre", M, 0, N, pre, d.ld_pre);
+    if (!to_workspace(a[7], &work, &bytes)) return NULL;
+    STREAM(8);
+    d.rows = (int32_t)M; d.in_features = (int32_t)K; d.out_features = (int32_t)N; d.activation = act;
+    CALL(hts_linear(&d, x, w, bias, res, y, pre, work, bytes, stream), "hts_linear");
+}
+FN(linear_gradient)
+{
+    (void)self;
+    ARGS(10);
+    int32_t dtype;
+    int64_t T, M, K, N, bytes;
+    hts_linear_desc d = {0};
+    void *x, *w, *pre, *dy, *dx, *dw = NULL, *work;
+    float *db;
+    if (!to_lead(a[0], "x", 1, &dtype, &T, &M, &K) || !to_size(a[1], "w", BF16_T, 2, 0, &N)) return NULL;
+    dtype = BF16_T;
+    ROWS(a[0], "x", M, 0, K, x, d.ld_x);
+    DENSE(a[1], "w", BF16_T, N, K, 0, w);
+    ROWS(a[2], "pre", M, 0, N, pre, d.ld_pre);
+    ROWS(a[3], "dy", M, 0, N, dy, d.ld_dy);
+    I32(act, 4);
+    ROWS(a[5], "dx", M, 0, K, dx, d.ld_dx);
+    if (a[6] != Py_None) {
+        Seen v;
+        if (!look(a[6], "dw", -1, &v)) return NULL;
+        d.dw_dtype = v.type;
+        DENSE(a[6], "dw", v.type, N, K, 0, dw);
+    }
+    DENSE(a[7], "dbias", F32_T, N, 0, 0, db);
+    if (!to_workspace(a[8], &work, &bytes)) return NULL;
+    STREAM(9);
+    d.rows = (int32_t)M; d.in_features = (int32_t)K; d.out_features = (int32_t)N; d.activation = act;
+    CALL(hts_linear_gradient(&d, x, w, pre, dy, dx, dw, db, work, bytes, stream), "hts_linear_gradient");
+}
+
 static PyObject *init(PyObject *self, PyObject *error)
 {
     (void)self;
@@ -493,7 +546,7 @@ static PyObject *init(PyObject *self, PyObject *error)
 static PyMethodDef kMethods[] = {
     M(policy_step), M(policy_step_host), M(policy_step_indexed), M(policy_evaluate), M(policy_gradient), M(policy_load_weights),
     M(a2c_terms), M(ppo_terms), M(delayed_update), M(gae), M(gae_host), M(vtrace), M(causal_conv), M(causal_conv_step), M(causal_conv_gradient),
-    M(selective_scan), M(selective_scan_step), M(selective_scan_gradient), {"init", init, METH_O, NULL}, {NULL, NULL, 0, NULL}};
+    M(selective_scan), M(selective_scan_step), M(selective_scan_gradient), M(linear), M(linear_gradient), {"init", init, METH_O, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", NULL, -1, kMethods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__native(void)

@@ -1,0 +1,670 @@
+// A dense layer with its epilogue, y = act(x w^T + bias) + residual, and its gradients, in bf16 on the tensor cores (tcgen05).
+//
+// Three products of one form, D[m, n] = sum over k of A[m, k] B[n, k]:
+//   y       A = x,  B = w              both with k along adjacent elements
+//   dx      A = dz, B = w              w has k (the layer's outputs) along its rows
+//   dw      A = dz, B = x              both have k (the batch's rows) along their rows
+// An operand with k along its rows is copied as it lies (64 rows x 64 columns a box) and described to the MMA as such, so that nothing
+// is transposed in memory.  dz = dy act'(pre) is taken beforehand in one pass that also sums it for dbias.
+//
+// Large products run on pairs of SMs, 256 x 256 outputs a pair, persistent, with two accumulators in tensor memory so that one
+// tile's epilogue runs under the next one's products.  A pair of SMs needs 64 bytes of operands from L2 per SM and tensor clock,
+// a 128 x 256 tile on a single SM 96, and L2 delivers about 50.  Few tiles (a step of few rows) are cut along k over
+// clusters of up to eight SMs: each forms a partial 128 x 64 tile, leaves it in its shared memory, and the cluster adds them in rank
+// order and runs the epilogue, in the same launch.  dw has few tiles and a long k: pairs take ranges of k and leave planes
+// of fp32 sums, which a second kernel adds in order.
+//
+// Sums are fp32; the tensor core cuts partial sums off where fp32 additions would round, up to one last place per 16 products, far below
+// the outputs' bf16.  All waits are bounded; a tile whose wait ran out is written as NaN.
+#include "recurrent.cuh"
+#include "tc_pair.cuh"
+#include "tc_host.cuh"
+
+namespace hts {
+using namespace tc;
+
+namespace {
+
+typedef __nv_bfloat16 bf16;
+constexpr int kBlockK = 64;                     // one 128-byte swizzle row
+
+bool make_bf16_map(CUtensorMap* m, const void* ptr, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {ld * 2};
+    const cuuint32_t box[2] = {64, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// What is done with the sums.
+struct Output {
+    int rows, cols;                             // valid extent
+    int activation;
+    int vec;                                    // elements that may be moved at once: 16, 8 or 1
+    int64_t ld_y, ld_pre, ld_res;
+    bf16 *y, *pre;                              // pre may be null
+    const bf16* residual;                       // or null
+    const float* bias;                          // or null
+    float* planes;                              // instead of y: fp32 sums [range][rows][cols]
+};
+enum Epilogue { LAYER, PLAIN, PLANES };         // all of it; rounded sums; fp32 sums
+
+__device__ __forceinline__ float activate(float v, int act)
+{
+    if (act == HTS_ACT_RELU) return v != v ? v : fmaxf(v, 0.f);
+    if (act == HTS_ACT_SILU) return silu(v);
+    if (act == HTS_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678f));
+    return v;
+}
+__device__ __forceinline__ float slope_of(float v, int act)
+{
+    if (act == HTS_ACT_RELU) return v > 0.f ? 1.f : 0.f;
+    if (act == HTS_ACT_SILU) return silu_slope(v);
+    if (act == HTS_ACT_GELU) return fmaf(v * 0.39894228f, exp2_approx(-0.5f * kLog2e * v * v), 0.5f * (1.f + erff(v * 0.70710678f)));
+    return 1.f;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// N neighbouring elements of a row, as many as are valid.
+template <int N>
+__device__ __forceinline__ void store_row(bf16* to, const float (&v)[N], int valid, int vec)
+{
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
+    if (N == 16 && vec == 16 && valid >= 16) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[N / 2 - 4]), "r"(w[N / 2 - 3]), "r"(w[N / 2 - 2]), "r"(w[N / 2 - 1]) : "memory");
+    } else if (vec >= 8 && valid >= N) {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) *reinterpret_cast<uint4*>(to + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < valid) to[i] = from_float<bf16>(v[i]);
+    }
+}
+template <int N>
+__device__ __forceinline__ void add_row(const bf16* from, float (&v)[N], int valid, int vec)
+{
+    if (vec >= 8 && valid >= N) {
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            const uint4 u = *reinterpret_cast<const uint4*>(from + 8 * i);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[8 * i + 2 * k] += __uint_as_float(w[k] << 16);
+                v[8 * i + 2 * k + 1] += __uint_as_float(w[k] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < valid) v[i] += to_float(from[i]);
+    }
+}
+// N sums of a row, from column `col` on; bias: of those columns.
+template <Epilogue EPI, int N>
+__device__ __forceinline__ void finish(const Output& o, int row, int col, float (&v)[N], const float* bias, int range)
+{
+    const int valid = o.cols - col;
+    if (row >= o.rows || valid <= 0) return;
+    if (EPI == PLANES) {
+        float* to = o.planes + ((size_t)range * o.rows + row) * o.cols + col;
+        if (o.vec > 1 && valid >= N) {
+#pragma unroll
+            for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < valid) to[i] = v[i];
+        }
+        return;
+    }
+    if (EPI == LAYER) {
+        if (bias)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += bias[i];
+        if (o.pre) store_row(o.pre + row * o.ld_pre + col, v, valid, o.vec);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = activate(v[i], o.activation);
+        if (o.residual) add_row(o.residual + row * o.ld_res + col, v, valid, o.vec);
+    }
+    store_row(o.y + row * o.ld_y + col, v, valid, o.vec);
+}
+
+// ---- pairs of SMs ----------------------------------------------------------------------------------------------------------
+constexpr int kPairThreads = 320;               // warp 0 copies, warp 1 issues, warps 2..9 epilogue (two per lane quarter)
+constexpr int kPairM = 256, kPairN = 256, kHalf = kPairN / 2;
+constexpr int kPairA = 128 * 128, kPairStage = kPairA + kHalf * 128, kPairStages = 6;
+constexpr int kPairSmem = 1024 + kPairStages * kPairStage;
+
+struct Work {
+    int m_tiles, n_tiles, ranges;               // of k, each of `blocks` blocks (the last may have fewer)
+    int blocks, all_blocks;
+};
+
+// One operand's tile of a block of k: `rows` M or N elements of this CTA from element `e0` on, k from k0.
+template <bool ROWS>
+__device__ __forceinline__ void pair_load(uint32_t dst, const CUtensorMap* map, int e0, int k0, uint32_t bar)
+{
+    if (ROWS) {                                 // boxes of 64 k rows x 64 elements
+        tma_load_2d_pair(dst, map, e0, k0, bar);
+        tma_load_2d_pair(dst + 8192, map, e0 + 64, k0, bar);
+    } else
+        tma_load_2d_pair(dst, map, k0, e0, bar);
+}
+template <bool ROWS>
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) { return ROWS ? smem_desc_rows(addr, 8192) : smem_desc_sw128(addr); }
+template <bool ROWS> constexpr uint32_t kStepK = ROWS ? 2048 / 16 : 32 / 16;        // descriptor units per 16 of k
+
+template <bool A_ROWS, bool B_ROWS, Epilogue EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
+linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Work wk, const Output o)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * kPairStages + 4];
+    uint64_t *full_bar = bars, *empty_bar = bars + kPairStages, *acc_full = empty_bar + kPairStages, *acc_empty = acc_full + 2;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    __shared__ __align__(16) float s_bias[2][kPairN];
+    volatile int* abortp = &abort_flag;
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;      // the same offset in both CTAs
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank();
+    if (warp == 0) {
+        if (lane < 2 * kPairStages + 4) mbar_init(&bars[lane], lane < 2 * kPairStages + 2 ? 1 : 16);
+        fence_barrier_init();
+    } else if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2 * kPairN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else if (warp == 2 && lane == 0) {
+        abort_flag = 0;
+        tma_prefetch_desc(&tmA);
+        tma_prefetch_desc(&tmB);
+    }
+    static_assert(2 * kPairStages + 4 <= 32, "a lane initialises one barrier");
+    tc_fence_before();
+    cluster_sync();                                      // of both CTAs' threads: the partner's barriers exist
+    tc_fence_after();
+    const uint32_t tmem_d = tmem_slot;
+    pdl_wait();
+    pdl_trigger();
+
+    const int pairs = gridDim.x / 2, work = wk.m_tiles * wk.n_tiles * wk.ranges;
+    // work item: n fastest, so that the pairs that run together share rows of A
+    auto item = [&](int w, int& m0, int& n0, int& range, int& k0, int& blocks) {
+        n0 = w % wk.n_tiles * kPairN;
+        m0 = w / wk.n_tiles % wk.m_tiles * kPairM;
+        range = w / wk.n_tiles / wk.m_tiles;
+        k0 = range * wk.blocks;
+        blocks = min(wk.blocks, wk.all_blocks - k0);
+    };
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            bool alive = true;
+            for (int w = blockIdx.x / 2; alive && w < work; w += pairs) {
+                int m0, n0, range, k0, blocks;
+                item(w, m0, n0, range, k0, blocks);
+                for (int b = 0; b < blocks; ++b, ++it) {
+                    const int st = it % kPairStages;
+                    if (it >= kPairStages && !mbar_wait(&empty_bar[st], ((uint32_t)(it / kPairStages) & 1u) ^ 1u, abortp, nullptr, 0)) { alive = false; break; }
+                    const uint32_t dst = base + st * kPairStage, bar = in_cta(&full_bar[st], 0);
+                    if (rank == 0) mbar_arrive_expect_tx(&full_bar[st], 2 * kPairStage);
+                    const int k = (k0 + b) * kBlockK;
+                    pair_load<A_ROWS>(dst, &tmA, m0 + rank * 128, k, bar);
+                    pair_load<B_ROWS>(dst + kPairA, &tmB, n0 + rank * kHalf, k, bar);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && elect_one()) {
+            constexpr uint32_t idesc = instr_desc_f16(1, kPairM, kPairN) | ((uint32_t)A_ROWS << 15) | ((uint32_t)B_ROWS << 16);
+            int it = 0, turn = 0;
+            bool alive = true;
+            for (int w = blockIdx.x / 2; alive && w < work; w += pairs, ++turn) {
+                int m0, n0, range, k0, blocks;
+                item(w, m0, n0, range, k0, blocks);
+                const int acc = turn & 1;
+                if (turn >= 2 && !mbar_wait(&acc_empty[acc], ((uint32_t)(turn >> 1) & 1u) ^ 1u, abortp, nullptr, 0)) break;
+                tc_fence_after();
+                for (int b = 0; b < blocks; ++b, ++it) {
+                    const int st = it % kPairStages;
+                    if (!mbar_wait(&full_bar[st], (uint32_t)(it / kPairStages) & 1u, abortp, nullptr, 0)) { alive = false; break; }
+                    tc_fence_after();
+                    const uint32_t a_addr = base + st * kPairStage;
+                    const uint64_t adesc = tile_desc<A_ROWS>(a_addr), bdesc = tile_desc<B_ROWS>(a_addr + kPairA);
+#pragma unroll
+                    for (int k = 0; k < kBlockK / 16; ++k)
+                        mma_f16_pair(tmem_d + acc * kPairN, adesc + k * kStepK<A_ROWS>, bdesc + k * kStepK<B_ROWS>, idesc, (b | k) != 0);
+                    mma_commit_pair(&empty_bar[st]);
+                }
+                if (alive) mma_commit_pair(&acc_full[acc]);
+            }
+        }
+    } else {
+        // epilogue warps 2..9: lane quarter warp % 4, columns [kHalf half, kHalf half + kHalf) of the tile
+        const int q = warp & 3, half = (warp - 2) >> 2, id = threadIdx.x - 64;
+        int turn = 0;
+        bool ok = true;
+        for (int w = blockIdx.x / 2; w < work; w += pairs, ++turn) {
+            int m0, n0, range, k0, blocks;
+            item(w, m0, n0, range, k0, blocks);
+            const int acc = turn & 1, row = m0 + rank * 128 + q * 32 + lane;
+            if (EPI == LAYER && o.bias) {       // the buffer of two tiles ago: every warp has passed the barrier of the last
+                s_bias[acc][id] = n0 + id < o.cols ? o.bias[n0 + id] : 0.f;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            }
+            ok = ok && mbar_wait_warp(&acc_full[acc], (uint32_t)(turn >> 1) & 1u, abortp, nullptr, 0);
+            tc_fence_after();
+            const uint32_t taddr = tmem_d + acc * kPairN + half * kHalf + ((uint32_t)(q * 32) << 16);
+#pragma unroll 1
+            for (int c = 0; c < kHalf; c += 32) {
+                uint32_t r[32];
+                tmem_ld_32x32(taddr + c, r);
+                tmem_ld_wait();
+                if (c + 32 == kHalf) {          // the accumulator is in registers: hand it back
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0 && w + 2 * pairs < work) arrive_cluster(in_cta(&acc_empty[acc], 0));     // what is waited for, and no more
+                }
+#pragma unroll
+                for (int hf = 0; hf < 32; hf += 16) {
+                    float v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = ok ? __uint_as_float(r[hf + i]) : __int_as_float(0x7fffffff);
+                    const int cc = half * kHalf + c + hf;
+                    finish<EPI, 16>(o, row, n0 + cc, v, EPI == LAYER && o.bias ? &s_bias[acc][cc] : nullptr, range);
+                }
+            }
+        }
+    }
+    if (*abortp) let_copies_land();
+    tc_fence_before();
+    __syncthreads();
+    // neither CTA leaves while the other's MMAs need its memory
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"(2 * kPairN) : "memory");
+}
+
+// ---- clusters along k -------------------------------------------------------------------------------------------------------
+constexpr int kSplitThreads = 192;              // warp 0 copies, warp 1 issues, warps 2..5 empty the accumulator; then all run the epilogue
+constexpr int kSplitN = 64, kSplitStages = 4, kSplitA = 128 * 128, kSplitStage = kSplitA + kSplitN * 128;
+constexpr int kPartialPitch = kSplitN + 4;      // floats: rows start four banks apart
+constexpr int kSplitSmem = 1024 + (kSplitStages * kSplitStage > 128 * kPartialPitch * 4 ? kSplitStages * kSplitStage : 128 * kPartialPitch * 4);
+
+template <bool B_ROWS, Epilogue EPI>
+__global__ void __launch_bounds__(kSplitThreads)
+linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Work wk, const Output o)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_bar[kSplitStages], empty_bar[kSplitStages], done_bar;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    volatile int* abortp = &abort_flag;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    float* partial = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank(), ranks = (int)cluster_size();
+    const int tile = blockIdx.x / ranks, n0 = tile % wk.n_tiles * kSplitN, m0 = tile / wk.n_tiles * 128;
+    const int k0 = rank * wk.blocks, blocks = max(0, min(wk.blocks, wk.all_blocks - k0));
+
+    if (warp == 0) {
+        if (lane < kSplitStages) { mbar_init(&full_bar[lane], 1); mbar_init(&empty_bar[lane], 1); }
+        if (lane == 0) mbar_init(&done_bar, 1);
+        fence_barrier_init();
+    } else if (warp == 1)
+        tmem_alloc(&tmem_slot, kSplitN);
+    else if (warp == 2 && lane == 0) {
+        abort_flag = 0;
+        tma_prefetch_desc(&tmA);
+        tma_prefetch_desc(&tmB);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_d = tmem_slot;
+    pdl_wait();
+    pdl_trigger();
+
+    if (warp == 0) {
+        if (lane == 0)
+            for (int b = 0; b < blocks; ++b) {
+                const int st = b % kSplitStages, k = (k0 + b) * kBlockK;
+                if (b >= kSplitStages && !mbar_wait(&empty_bar[st], ((uint32_t)(b / kSplitStages) & 1u) ^ 1u, abortp, nullptr, 0)) break;
+                mbar_arrive_expect_tx(&full_bar[st], kSplitStage);
+                uint8_t* dst = reinterpret_cast<uint8_t*>(partial) + st * kSplitStage;
+                tma_load_2d(dst, &tmA, k, m0, &full_bar[st]);
+                if (B_ROWS) tma_load_2d(dst + kSplitA, &tmB, n0, k, &full_bar[st]);
+                else tma_load_2d(dst + kSplitA, &tmB, k, n0, &full_bar[st]);
+            }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            constexpr uint32_t idesc = instr_desc_f16(1, 128, kSplitN) | ((uint32_t)B_ROWS << 16);
+            bool alive = true;
+            for (int b = 0; alive && b < blocks; ++b) {
+                const int st = b % kSplitStages;
+                if (!mbar_wait(&full_bar[st], (uint32_t)(b / kSplitStages) & 1u, abortp, nullptr, 0)) { alive = false; break; }
+                tc_fence_after();
+                const uint32_t a_addr = base + st * kSplitStage;
+                const uint64_t adesc = smem_desc_sw128(a_addr), bdesc = tile_desc<B_ROWS>(a_addr + kSplitA);
+#pragma unroll
+                for (int k = 0; k < kBlockK / 16; ++k) mma_f16_ss(tmem_d, adesc + k * kStepK<false>, bdesc + k * kStepK<B_ROWS>, idesc, (b | k) != 0);
+                mma_commit(&empty_bar[st]);
+            }
+            if (alive && blocks) mma_commit(&done_bar);
+        }
+    } else {
+        const int q = warp & 3, row = q * 32 + lane;
+        const bool ok = blocks == 0 || mbar_wait_warp(&done_bar, 0, abortp, nullptr, 0);
+        tc_fence_after();
+        if (!ok) let_copies_land();             // the partial sums' memory is the copies'
+#pragma unroll
+        for (int c = 0; c < kSplitN; c += 32) {
+            uint32_t r[32];
+            tmem_ld_32x32(tmem_d + c + ((uint32_t)(q * 32) << 16), r);
+            tmem_ld_wait();
+            if (m0 + row < o.rows)
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    float4 v = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                    if (blocks == 0) v = make_float4(0, 0, 0, 0);
+                    if (!ok) v.x = v.y = v.z = v.w = __int_as_float(0x7fffffff);
+                    *reinterpret_cast<float4*>(partial + row * kPartialPitch + c + i) = v;
+                }
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    cluster_sync();
+    // eight columns of a row to a thread, the cluster's partial sums in rank order
+    const int rows = min(128, o.rows - m0);
+    for (int e = rank * kSplitThreads + threadIdx.x; e < rows * (kSplitN / 8); e += ranks * kSplitThreads) {
+        const int row = e / (kSplitN / 8), c = e % (kSplitN / 8) * 8;
+        float v[8] = {}, bias[8];
+        for (int i = 0; i < ranks; ++i) {
+            const uint32_t at = in_cta(partial + row * kPartialPitch + c, i);
+            const float4 lo = load_cluster(at), hi = load_cluster(at + 16);
+            v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w; v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+        }
+        if (EPI == LAYER && o.bias)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) bias[i] = n0 + c + i < o.cols ? o.bias[n0 + c + i] : 0.f;
+        finish<EPI, 8>(o, m0 + row, n0 + c, v, EPI == LAYER && o.bias ? bias : nullptr, 0);
+    }
+    cluster_sync();                             // nobody leaves while its sums are read
+    if (warp == 1) tmem_dealloc(tmem_d, kSplitN);
+}
+
+// ---- around the products ----------------------------------------------------------------------------------------------------
+// Rows as the copies need them: dense, a multiple of eight elements long.
+__global__ void __launch_bounds__(256) pack_kernel(const bf16* from, int64_t ld, int64_t rows, int cols, int padded, bf16* to)
+{
+    pdl_wait();
+    pdl_trigger();
+    for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < rows * padded; id += (int64_t)gridDim.x * 256) {
+        const int c = (int)(id % padded);
+        to[id] = c < cols ? from[id / padded * ld + c] : from_float<bf16>(0.f);
+    }
+}
+
+// dz = dy act'(pre), rounded, and its sums over 64 rows: part[row block][cols].  V channels a thread.
+constexpr int kSumRows = 64;
+template <int V>
+__global__ void __launch_bounds__(256) dz_kernel(const bf16* dy, int64_t ld_dy, const bf16* pre, int64_t ld_pre, int rows, int cols, int act, bf16* dz, int ld_dz,
+                                                 float* part)
+{
+    pdl_wait();
+    pdl_trigger();
+    __shared__ float sums[8][32 * V];
+    const int across = (cols + 32 * V - 1) / (32 * V), c = (int)(blockIdx.x % across) * 32 * V + threadIdx.x * V, block = blockIdx.x / across;
+    float sum[V] = {};
+    if (c < cols)
+#pragma unroll 4
+        for (int i = threadIdx.y; i < kSumRows; i += 8) {
+            const int64_t row = (int64_t)block * kSumRows + i;
+            if (row >= rows) break;
+            const Vec<bf16, V> g = load_vec<V>(dy + row * ld_dy + c);
+            float v[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = to_float(g.v[k]);
+            if (pre) {
+                const Vec<bf16, V> u = load_vec<V>(pre + row * ld_pre + c);
+#pragma unroll
+                for (int k = 0; k < V; ++k) v[k] *= slope_of(to_float(u.v[k]), act);
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) sum[k] += v[k];
+            if (dz) store_vec<V>(dz + row * ld_dz + c, v);
+        }
+    if (!part) return;
+#pragma unroll
+    for (int k = 0; k < V; ++k) sums[threadIdx.y][threadIdx.x * V + k] = sum[k];
+    __syncthreads();
+    for (int e = threadIdx.y * 32 + threadIdx.x; e < 32 * V; e += 256) {
+        float a = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a += sums[i][e];
+        const int col = (int)(blockIdx.x % across) * 32 * V + e;
+        if (col < cols) part[(size_t)block * cols + col] = a;
+    }
+}
+
+// Planes of sums added in order.
+template <typename T>
+__global__ void __launch_bounds__(256) planes_kernel(const float* planes, int count, int64_t size, T* out)
+{
+    pdl_wait();
+    pdl_trigger();
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= size) return;
+    float v = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) v += planes[i * size + id];
+    out[id] = from_float<T>(v);
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------------------------
+int padded(int cols) { return (cols + 7) / 8 * 8; }
+bool as_is(const void* p, int64_t ld) { return aligned_to(p, 16) && ld % 8 == 0; }
+
+struct Operand { const bf16* p; int64_t ld; };
+// The operand itself, or a copy of it where its rows do not start on 16-byte boundaries.
+hts_status laid_out(const bf16* p, int64_t ld, int rows, int cols, bf16* copy, Operand* out, cudaStream_t s)
+{
+    *out = {p, ld};
+    if (as_is(p, ld)) return HTS_OK;
+    const int64_t blocks = ceil_div((int64_t)rows * padded(cols), 1024);
+    HTS_CUDA(launch_pdl(pack_kernel, dim3((unsigned)(blocks < 16 * kCoreSms ? blocks : 16 * kCoreSms)), dim3(256), 0, s, p, ld, (int64_t)rows, cols, padded(cols), copy));
+    note_launch();
+    *out = {copy, padded(cols)};
+    return HTS_OK;
+}
+
+template <bool A_ROWS, bool B_ROWS, Epilogue EPI>
+hts_status launch_pairs(const Operand& a, const Operand& b, int M, int N, int K, int ranges, const Output& o, cudaStream_t s)
+{
+    CUtensorMap ma, mb;
+    if (!(A_ROWS ? make_bf16_map(&ma, a.p, K, M, a.ld, 64) : make_bf16_map(&ma, a.p, M, K, a.ld, 128)) ||
+        !(B_ROWS ? make_bf16_map(&mb, b.p, K, N, b.ld, 64) : make_bf16_map(&mb, b.p, N, K, b.ld, kHalf)))
+        return HTS_ERR_CUDA;
+    Work w{(int)ceil_div(M, kPairM), (int)ceil_div(N, kPairN), ranges, 0, (int)ceil_div(K, kBlockK)};
+    w.blocks = (int)ceil_div(w.all_blocks, ranges);
+    static OncePerDevice allowed;
+    HTS_CUDA(allow_shared(linear_pair_kernel<A_ROWS, B_ROWS, EPI>, allowed));
+    const int64_t work = (int64_t)w.m_tiles * w.n_tiles * ranges, pairs = device_sm_count(device_slot()) / 2;
+    HTS_CUDA(launch_pdl(linear_pair_kernel<A_ROWS, B_ROWS, EPI>, dim3((unsigned)(2 * (work < pairs ? work : pairs))), dim3(kPairThreads), (size_t)kPairSmem, s, ma, mb, w, o));
+    note_launch();
+    return HTS_OK;
+}
+template <bool B_ROWS, Epilogue EPI>
+hts_status launch_split(const Operand& a, const Operand& b, int M, int N, int K, const Output& o, cudaStream_t s)
+{
+    CUtensorMap ma, mb;
+    if (!make_bf16_map(&ma, a.p, M, K, a.ld, 128) || !(B_ROWS ? make_bf16_map(&mb, b.p, K, N, b.ld, 64) : make_bf16_map(&mb, b.p, N, K, b.ld, kSplitN))) return HTS_ERR_CUDA;
+    Work w{(int)ceil_div(M, 128), (int)ceil_div(N, kSplitN), 1, 0, (int)ceil_div(K, kBlockK)};
+    const int64_t tiles = (int64_t)w.m_tiles * w.n_tiles;
+    int ranks = 8;
+    while (ranks > 1 && (tiles * ranks > kCoreSms || ranks > w.all_blocks)) ranks /= 2;
+    w.blocks = (int)ceil_div(w.all_blocks, ranks);
+    static OncePerDevice allowed;
+    auto kernel = linear_split_kernel<B_ROWS, EPI>;
+    HTS_CUDA(allow_shared(kernel, allowed));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * ranks)); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = kSplitSmem; cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ranks; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    HTS_CUDA(cudaLaunchKernelEx(&cfg, kernel, ma, mb, w, o));
+    note_launch();
+    return HTS_OK;
+}
+// Pairs of SMs where their 256 x 256 tiles keep half of the device busy, else 128 x 64 tiles cut along k.
+template <bool B_ROWS, Epilogue EPI>
+hts_status launch_product(const Operand& a, const Operand& b, int M, int N, int K, const Output& o, cudaStream_t s)
+{
+    if (ceil_div(M, kPairM) * ceil_div(N, kPairN) * 4 >= kCoreSms) return launch_pairs<false, B_ROWS, EPI>(a, b, M, N, K, 1, o, s);
+    return launch_split<B_ROWS, EPI>(a, b, M, N, K, o, s);
+}
+
+int vec_of(std::initializer_list<const void*> pointers, std::initializer_list<int64_t> strides)
+{
+    int vec = 16;
+    for (const void* p : pointers) vec = aligned_to(p, 32) ? vec : aligned_to(p, 16) && vec >= 8 ? 8 : 1;
+    for (int64_t l : strides) vec = l % 16 == 0 ? vec : l % 8 == 0 && vec >= 8 ? 8 : 1;
+    return vec;
+}
+
+// Ranges of dw's long k: enough for every pair of SMs, eight blocks of k each at least.
+int dw_ranges(int M, int K, int N)
+{
+    const int64_t tiles = ceil_div(N, kPairM) * ceil_div(K, kPairN), blocks = ceil_div(M, kBlockK);
+    int64_t r = kCoreSms / 2 / tiles;
+    if (r > blocks / 8) r = blocks / 8;
+    if (r < 1) r = 1;
+    return (int)ceil_div(blocks, ceil_div(blocks, r));           // no range is empty
+}
+struct LinearPlan { size_t x, w, dz, sums, planes, bytes; int ranges; };
+LinearPlan linear_plan(int M, int K, int N, bool gradient)
+{
+    LinearPlan q{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t was = at; at += round256(bytes); return was; };
+    q.x = take((size_t)M * padded(K) * 2);
+    q.w = take((size_t)N * padded(K) * 2);
+    if (gradient) {
+        q.ranges = dw_ranges(M, K, N);
+        q.dz = take((size_t)M * padded(N) * 2);
+        q.sums = take((size_t)ceil_div(M, kSumRows) * N * 4);
+        q.planes = take((size_t)q.ranges * N * K * 4);
+    }
+    q.bytes = at;
+    return q;
+}
+bool bad(const hts_linear_desc* d)
+{
+    return !d || d->rows < 1 || d->in_features < 1 || d->out_features < 1 || d->activation < HTS_ACT_NONE || d->activation > HTS_ACT_GELU ||
+           d->ld_x < d->in_features || ceil_div(d->rows, 128) * ceil_div(d->out_features, kSplitN) > INT32_MAX / 8 ||
+           ceil_div(d->rows, 128) * ceil_div(d->in_features, kSplitN) > INT32_MAX / 8 || (int64_t)d->out_features * d->in_features > ((int64_t)1 << 38);
+}
+
+}  // namespace
+}  // namespace hts
+
+using namespace hts;
+
+extern "C" int64_t hts_linear_workspace(int32_t rows, int32_t in_features, int32_t out_features, int32_t gradient)
+{
+    if (rows < 1 || in_features < 1 || out_features < 1) return 0;
+    return (int64_t)linear_plan(rows, in_features, out_features, gradient != 0).bytes;
+}
+
+extern "C" hts_status hts_linear(const hts_linear_desc* d, const void* x, const void* w, const float* bias, const void* residual, void* y, void* pre, void* workspace,
+                                 int64_t workspace_bytes, void* stream)
+{
+    if (bad(d) || !x || !w || !y || d->ld_y < d->out_features || (residual && d->ld_residual < d->out_features) || (pre && d->ld_pre < d->out_features) || y == x || y == w ||
+        (pre && (pre == x || pre == w || pre == y || pre == residual)))
+        return HTS_ERR_INVALID_ARG;
+    const int M = d->rows, K = d->in_features, N = d->out_features;
+    const LinearPlan q = linear_plan(M, K, N, false);
+    if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < (int64_t)q.bytes) return HTS_ERR_INVALID_ARG;
+    char* ws = (char*)workspace;
+    const cudaStream_t s = (cudaStream_t)stream;
+    Operand a, b;
+    hts_status st = laid_out((const bf16*)x, d->ld_x, M, K, (bf16*)(ws + q.x), &a, s);
+    if (st == HTS_OK) st = laid_out((const bf16*)w, K, N, K, (bf16*)(ws + q.w), &b, s);
+    if (st != HTS_OK) return st;
+    Output o{};
+    o.rows = M; o.cols = N; o.activation = d->activation; o.ld_y = d->ld_y; o.ld_pre = d->ld_pre; o.ld_res = d->ld_residual;
+    o.y = (bf16*)y; o.pre = (bf16*)pre; o.residual = (const bf16*)residual; o.bias = bias;
+    o.vec = vec_of({y, pre, residual}, {d->ld_y, pre ? d->ld_pre : 0, residual ? d->ld_residual : 0});
+    return launch_product<false, LAYER>(a, b, M, N, K, o, s);
+}
+
+extern "C" hts_status hts_linear_gradient(const hts_linear_desc* d, const void* x, const void* w, const void* pre, const void* dy, void* dx, void* dw, float* dbias,
+                                          void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (bad(d) || !x || !w || !dy || d->ld_dy < d->out_features || (dx && d->ld_dx < d->in_features) || (!dx && !dw && !dbias) ||
+        (d->activation != HTS_ACT_NONE && (!pre || d->ld_pre < d->out_features)) || (dw && d->dw_dtype != HTS_DTYPE_FP32 && d->dw_dtype != HTS_DTYPE_BF16) ||
+        (dx && (dx == x || dx == dy || dx == w || dx == pre)) || (dw && (dw == w || dw == x || dw == dy)))
+        return HTS_ERR_INVALID_ARG;
+    const int M = d->rows, K = d->in_features, N = d->out_features;
+    const LinearPlan q = linear_plan(M, K, N, true);
+    if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < (int64_t)q.bytes) return HTS_ERR_INVALID_ARG;
+    char* ws = (char*)workspace;
+    const cudaStream_t s = (cudaStream_t)stream;
+    const bool act = d->activation != HTS_ACT_NONE, copy = act || !as_is(dy, d->ld_dy);
+    if (!act) pre = nullptr;
+    Operand g{(const bf16*)dy, d->ld_dy}, a, b;
+    if (dbias || (copy && (dx || dw))) {
+        bf16* dz = copy && (dx || dw) ? (bf16*)(ws + q.dz) : nullptr;
+        float* part = dbias ? (float*)(ws + q.sums) : nullptr;
+        const bool wide = N % 8 == 0 && as_is(dy, d->ld_dy) && (!pre || as_is(pre, d->ld_pre));
+        const int64_t blocks = ceil_div(M, kSumRows) * ceil_div(N, wide ? 256 : 32);
+        if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
+        HTS_CUDA(launch_pdl(wide ? dz_kernel<8> : dz_kernel<1>, dim3((unsigned)blocks), dim3(32, 8), 0, s, (const bf16*)dy, d->ld_dy, (const bf16*)pre, d->ld_pre, M, N,
+                            d->activation, dz, padded(N), part));
+        note_launch();
+        if (dz) g = {dz, padded(N)};
+        if (dbias) {
+            const hts_status st = launch_column_sums({part, ceil_div(M, kSumRows), N, N, N, 1, dbias, nullptr, N, nullptr}, s);
+            if (st != HTS_OK) return st;
+        }
+    }
+    if (dx) {
+        hts_status st = laid_out((const bf16*)w, K, N, K, (bf16*)(ws + q.w), &b, s);
+        if (st != HTS_OK) return st;
+        Output o{};
+        o.rows = M; o.cols = K; o.ld_y = d->ld_dx; o.y = (bf16*)dx; o.vec = vec_of({dx}, {d->ld_dx});
+        st = launch_product<true, PLAIN>(g, b, M, K, N, o, s);
+        if (st != HTS_OK) return st;
+    }
+    if (dw) {
+        hts_status st = laid_out((const bf16*)x, d->ld_x, M, K, (bf16*)(ws + q.x), &a, s);
+        if (st != HTS_OK) return st;
+        Output o{};
+        o.rows = N; o.cols = K; o.planes = (float*)(ws + q.planes); o.vec = K % 4 == 0 ? 8 : 1;
+        st = launch_pairs<true, true, PLANES>(g, a, N, K, M, q.ranges, o, s);
+        if (st != HTS_OK) return st;
+        const int64_t size = (int64_t)N * K;
+        const dim3 grid((unsigned)ceil_div(size, 256));
+        if (d->dw_dtype == HTS_DTYPE_FP32) HTS_CUDA(launch_pdl(planes_kernel<float>, grid, dim3(256), 0, s, (const float*)o.planes, q.ranges, size, (float*)dw));
+        else HTS_CUDA(launch_pdl(planes_kernel<bf16>, grid, dim3(256), 0, s, (const float*)o.planes, q.ranges, size, (bf16*)dw));
+        note_launch();
+    }
+    return HTS_OK;
+}
