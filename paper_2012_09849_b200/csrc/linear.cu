@@ -112,6 +112,10 @@ __device__ __forceinline__ void add_row(const bf16* from, float (&v)[N], int val
             if (i < valid) v[i] += to_float(from[i]);
     }
 }
+__device__ __forceinline__ void store_turn(uint32_t at, const float (&v)[8])
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(pack2(v[0], v[1])), "r"(pack2(v[2], v[3])), "r"(pack2(v[4], v[5])), "r"(pack2(v[6], v[7])) : "memory");
+}
 // N sums of a row, from column `col` on; bias: of those columns.
 template <Epilogue EPI, int N>
 __device__ __forceinline__ void finish(const Output& o, int row, int col, float (&v)[N], const float* bias, int range)
@@ -143,10 +147,13 @@ __device__ __forceinline__ void finish(const Output& o, int row, int col, float 
 }
 
 // ---- pairs of SMs ----------------------------------------------------------------------------------------------------------
-constexpr int kPairThreads = 320;               // warp 0 copies, warp 1 issues, warps 2..9 epilogue (two per lane quarter)
+constexpr int kPairWarps = 8, kPairThreads = 64 + 32 * kPairWarps;    // warp 0 copies, warp 1 issues, the others run the epilogue
 constexpr int kPairM = 256, kPairN = 256, kHalf = kPairN / 2;
-constexpr int kPairA = 128 * 128, kPairStage = kPairA + kHalf * 128, kPairStages = 6;
-constexpr int kPairSmem = 1024 + kPairStages * kPairStage;
+constexpr int kPairA = 128 * 128, kPairStage = kPairA + kHalf * 128;
+constexpr int kTurn = 32 * 128;                 // a warp's box of outputs on its way to memory: 32 rows x 64 columns
+template <Epilogue EPI> constexpr int kTurns = EPI == LAYER ? 2 : EPI == PLAIN ? 1 : 0;       // boxes of a warp
+template <Epilogue EPI> constexpr int kPairStages = 6 - kTurns<EPI>;
+template <Epilogue EPI> constexpr int kPairSmem = 1024 + kPairStages<EPI> * kPairStage + kPairWarps * kTurns<EPI> * kTurn;
 
 struct Work {
     int m_tiles, n_tiles, ranges;               // of k, each of `blocks` blocks (the last may have fewer)
@@ -169,11 +176,13 @@ template <bool ROWS> constexpr uint32_t kStepK = ROWS ? 2048 / 16 : 32 / 16;    
 
 template <bool A_ROWS, bool B_ROWS, Epilogue EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
-linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Work wk, const Output o)
+linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmY,
+                   const __grid_constant__ CUtensorMap tmPre, const Work wk, const Output o)
 {
+    constexpr int NST = kPairStages<EPI>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * kPairStages + 4];
-    uint64_t *full_bar = bars, *empty_bar = bars + kPairStages, *acc_full = empty_bar + kPairStages, *acc_empty = acc_full + 2;
+    __shared__ uint64_t bars[2 * NST + 4];
+    uint64_t *full_bar = bars, *empty_bar = bars + NST, *acc_full = empty_bar + NST, *acc_empty = acc_full + 2;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     __shared__ __align__(16) float s_bias[2][kPairN];
@@ -183,7 +192,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank();
     if (warp == 0) {
-        if (lane < 2 * kPairStages + 4) mbar_init(&bars[lane], lane < 2 * kPairStages + 2 ? 1 : 16);
+        if (lane < 2 * NST + 4) mbar_init(&bars[lane], lane < 2 * NST + 2 ? 1 : 2 * kPairWarps);
         fence_barrier_init();
     } else if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2 * kPairN) : "memory");
@@ -193,7 +202,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         tma_prefetch_desc(&tmA);
         tma_prefetch_desc(&tmB);
     }
-    static_assert(2 * kPairStages + 4 <= 32, "a lane initialises one barrier");
+    static_assert(2 * NST + 4 <= 32, "a lane initialises one barrier");
     tc_fence_before();
     cluster_sync();                                      // of both CTAs' threads: the partner's barriers exist
     tc_fence_after();
@@ -218,8 +227,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 int m0, n0, range, k0, blocks;
                 item(w, m0, n0, range, k0, blocks);
                 for (int b = 0; b < blocks; ++b, ++it) {
-                    const int st = it % kPairStages;
-                    if (it >= kPairStages && !mbar_wait(&empty_bar[st], ((uint32_t)(it / kPairStages) & 1u) ^ 1u, abortp, nullptr, 0)) { alive = false; break; }
+                    const int st = it % NST;
+                    if (it >= NST && !mbar_wait(&empty_bar[st], ((uint32_t)(it / NST) & 1u) ^ 1u, abortp, nullptr, 0)) { alive = false; break; }
                     const uint32_t dst = base + st * kPairStage, bar = in_cta(&full_bar[st], 0);
                     if (rank == 0) mbar_arrive_expect_tx(&full_bar[st], 2 * kPairStage);
                     const int k = (k0 + b) * kBlockK;
@@ -240,8 +249,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 if (turn >= 2 && !mbar_wait(&acc_empty[acc], ((uint32_t)(turn >> 1) & 1u) ^ 1u, abortp, nullptr, 0)) break;
                 tc_fence_after();
                 for (int b = 0; b < blocks; ++b, ++it) {
-                    const int st = it % kPairStages;
-                    if (!mbar_wait(&full_bar[st], (uint32_t)(it / kPairStages) & 1u, abortp, nullptr, 0)) { alive = false; break; }
+                    const int st = it % NST;
+                    if (!mbar_wait(&full_bar[st], (uint32_t)(it / NST) & 1u, abortp, nullptr, 0)) { alive = false; break; }
                     tc_fence_after();
                     const uint32_t a_addr = base + st * kPairStage;
                     const uint64_t adesc = tile_desc<A_ROWS>(a_addr), bdesc = tile_desc<B_ROWS>(a_addr + kPairA);
@@ -254,41 +263,85 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             }
         }
     } else {
-        // epilogue warps 2..9: lane quarter warp % 4, columns [kHalf half, kHalf half + kHalf) of the tile
-        const int q = warp & 3, half = (warp - 2) >> 2, id = threadIdx.x - 64;
+        // epilogue warps: lane quarter warp % 4, a share of the tile's columns
+        constexpr int COLS = kPairN / (kPairWarps / 4);
+        const int q = warp & 3, share = (warp - 2) >> 2, id = threadIdx.x - 64;
+        const uint32_t turn_smem = base + NST * kPairStage + (warp - 2) * kTurns<EPI> * kTurn;
         int turn = 0;
         bool ok = true;
+        auto bias_of = [&](int w) {             // this thread's column of a tile; asked for a tile ahead
+            const int col = w % wk.n_tiles * kPairN + id;
+            return EPI == LAYER && o.bias && w < work && id < kPairN && col < o.cols ? o.bias[col] : 0.f;
+        };
+        float next_bias = bias_of(blockIdx.x / 2);
         for (int w = blockIdx.x / 2; w < work; w += pairs, ++turn) {
             int m0, n0, range, k0, blocks;
             item(w, m0, n0, range, k0, blocks);
             const int acc = turn & 1, row = m0 + rank * 128 + q * 32 + lane;
             if (EPI == LAYER && o.bias) {       // the buffer of two tiles ago: every warp has passed the barrier of the last
-                s_bias[acc][id] = n0 + id < o.cols ? o.bias[n0 + id] : 0.f;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (id < kPairN) s_bias[acc][id] = next_bias;
+                next_bias = bias_of(w + pairs);
+                asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairWarps) : "memory");
             }
             ok = ok && mbar_wait_warp(&acc_full[acc], (uint32_t)(turn >> 1) & 1u, abortp, nullptr, 0);
             tc_fence_after();
-            const uint32_t taddr = tmem_d + acc * kPairN + half * kHalf + ((uint32_t)(q * 32) << 16);
+            const uint32_t taddr = tmem_d + acc * kPairN + share * COLS + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1
-            for (int c = 0; c < kHalf; c += 32) {
-                uint32_t r[32];
-                tmem_ld_32x32(taddr + c, r);
+            for (int c = 0; c < COLS; c += 64) {
+                uint32_t r[64];
+                tmem_ld_32x32(taddr + c, reinterpret_cast<uint32_t(&)[32]>(r[0]));
+                tmem_ld_32x32(taddr + c + 32, reinterpret_cast<uint32_t(&)[32]>(r[32]));
                 tmem_ld_wait();
-                if (c + 32 == kHalf) {          // the accumulator is in registers: hand it back
+                if (c + 64 == COLS) {           // the accumulator is in registers: hand it back
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0 && w + 2 * pairs < work) arrive_cluster(in_cta(&acc_empty[acc], 0));     // what is waited for, and no more
+                    if (lane == 0 && w + 2 * pairs < work) arrive_cluster_relaxed(in_cta(&acc_empty[acc], 0));     // what is waited for, and no more
                 }
+                if (!ok)
 #pragma unroll
-                for (int hf = 0; hf < 32; hf += 16) {
-                    float v[16];
+                    for (int i = 0; i < 64; ++i) r[i] = 0x7fffffff;
+                const int cc = share * COLS + c, valid = o.cols - n0 - cc;
+                const float* bias = EPI == LAYER && o.bias ? &s_bias[acc][cc] : nullptr;
+                if (EPI != PLANES && o.vec >= 8) {
+                    // rounded into a box in the copies' 128-byte swizzle, a row per lane, and from there to memory in whole lines
+                    if (lane == 0) tma_store_wait_read();
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = ok ? __uint_as_float(r[hf + i]) : __int_as_float(0x7fffffff);
-                    const int cc = half * kHalf + c + hf;
-                    finish<EPI, 16>(o, row, n0 + cc, v, EPI == LAYER && o.bias ? &s_bias[acc][cc] : nullptr, range);
-                }
+                    for (int g = 0; g < 8; ++g) {
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[8 * g + i]);
+                        const uint32_t at = turn_smem + lane * 128 + ((g ^ (lane & 7)) * 16);
+                        if (EPI == LAYER) {
+                            if (bias) {
+                                const float4 lo = *reinterpret_cast<const float4*>(bias + 8 * g), hi = *reinterpret_cast<const float4*>(bias + 8 * g + 4);
+                                v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w; v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+                            }
+                            if (o.pre) store_turn(at + kTurn, v);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], o.activation);
+                            if (o.residual && row < o.rows && 8 * g < valid) add_row(o.residual + row * o.ld_res + n0 + cc + 8 * g, v, valid - 8 * g, o.vec);
+                        }
+                        store_turn(at, v);
+                    }
+                    fence_async_proxy();
+                    __syncwarp();
+                    if (lane == 0 && valid > 0) {
+                        tma_store_2d(&tmY, turn_smem, n0 + cc, row);
+                        if (EPI == LAYER && o.pre) tma_store_2d(&tmPre, turn_smem + kTurn, n0 + cc, row);
+                        tma_store_commit();
+                    }
+                } else
+#pragma unroll
+                    for (int g = 0; g < 64; g += 16) {
+                        float v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[g + i]);
+                        finish<EPI, 16>(o, row, n0 + cc + g, v, bias ? bias + g : nullptr, range);
+                    }
             }
         }
+        if (lane == 0) tma_store_wait();
     }
     if (*abortp) let_copies_land();
     tc_fence_before();
@@ -495,7 +548,10 @@ hts_status laid_out(const bf16* p, int64_t ld, int rows, int cols, bf16* copy, O
 template <bool A_ROWS, bool B_ROWS, Epilogue EPI>
 hts_status launch_pairs(const Operand& a, const Operand& b, int M, int N, int K, int ranges, const Output& o, cudaStream_t s)
 {
-    CUtensorMap ma, mb;
+    CUtensorMap ma, mb, my{}, mp{};
+    if (EPI != PLANES && o.vec >= 8 &&
+        (!make_bf16_map(&my, o.y, M, N, o.ld_y, 32) || (o.pre && !make_bf16_map(&mp, o.pre, M, N, o.ld_pre, 32))))
+        return HTS_ERR_CUDA;
     if (!(A_ROWS ? make_bf16_map(&ma, a.p, K, M, a.ld, 64) : make_bf16_map(&ma, a.p, M, K, a.ld, 128)) ||
         !(B_ROWS ? make_bf16_map(&mb, b.p, K, N, b.ld, 64) : make_bf16_map(&mb, b.p, N, K, b.ld, kHalf)))
         return HTS_ERR_CUDA;
@@ -504,7 +560,7 @@ hts_status launch_pairs(const Operand& a, const Operand& b, int M, int N, int K,
     static OncePerDevice allowed;
     HTS_CUDA(allow_shared(linear_pair_kernel<A_ROWS, B_ROWS, EPI>, allowed));
     const int64_t work = (int64_t)w.m_tiles * w.n_tiles * ranges, pairs = device_sm_count(device_slot()) / 2;
-    HTS_CUDA(launch_pdl(linear_pair_kernel<A_ROWS, B_ROWS, EPI>, dim3((unsigned)(2 * (work < pairs ? work : pairs))), dim3(kPairThreads), (size_t)kPairSmem, s, ma, mb, w, o));
+    HTS_CUDA(launch_pdl(linear_pair_kernel<A_ROWS, B_ROWS, EPI>, dim3((unsigned)(2 * (work < pairs ? work : pairs))), dim3(kPairThreads), (size_t)kPairSmem<EPI>, s, ma, mb, my, mp, w, o));
     note_launch();
     return HTS_OK;
 }
