@@ -53,18 +53,36 @@ struct Output {
 };
 enum Epilogue { LAYER, PLAIN, PLANES };         // all of it; rounded sums; fp32 sums
 
+// The normal distribution's function at v, and exp(-v^2 / 2): erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2), t = 1 / (1 + p x), for x >= 0
+// (Abramowitz and Stegun 7.1.26: off by 1.5e-7 at most, and no difference of near numbers where v is negative).
+__device__ __forceinline__ float normal_cdf(float v, float& bell)
+{
+    const float x = fabsf(v) * 0.70710678f, t = rcp_approx(fmaf(0.3275911f, x, 1.f));
+    bell = exp2_approx(-kLog2e * x * x);
+    float r = fmaf(1.061405429f, t, -1.453152027f);
+    r = fmaf(r, t, 1.421413741f);
+    r = fmaf(r, t, -0.284496736f);
+    r = fmaf(r, t, 0.254829592f);
+    const float tail = 0.5f * r * t * bell;
+    return v < 0.f ? tail : 1.f - tail;
+}
 __device__ __forceinline__ float activate(float v, int act)
 {
+    float bell;
     if (act == HTS_ACT_RELU) return v != v ? v : fmaxf(v, 0.f);
     if (act == HTS_ACT_SILU) return silu(v);
-    if (act == HTS_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678f));
+    if (act == HTS_ACT_GELU) return v * normal_cdf(v, bell);
     return v;
 }
 __device__ __forceinline__ float slope_of(float v, int act)
 {
+    float bell;
     if (act == HTS_ACT_RELU) return v > 0.f ? 1.f : 0.f;
     if (act == HTS_ACT_SILU) return silu_slope(v);
-    if (act == HTS_ACT_GELU) return fmaf(v * 0.39894228f, exp2_approx(-0.5f * kLog2e * v * v), 0.5f * (1.f + erff(v * 0.70710678f)));
+    if (act == HTS_ACT_GELU) {
+        const float c = normal_cdf(v, bell);
+        return fmaf(v * 0.39894228f, bell, c);
+    }
     return 1.f;
 }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi)
@@ -114,7 +132,18 @@ __device__ __forceinline__ void add_row(const bf16* from, float (&v)[N], int val
 }
 __device__ __forceinline__ void store_turn(uint32_t at, const float (&v)[8])
 {
-    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(pack2(v[0], v[1])), "r"(pack2(v[2], v[3])), "r"(pack2(v[4], v[5])), "r"(pack2(v[6], v[7])) : "memory");
+    // no "memory": what reads it is behind a fence that has it, and the loads of the next columns may come first
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(pack2(v[0], v[1])), "r"(pack2(v[2], v[3])), "r"(pack2(v[4], v[5])), "r"(pack2(v[6], v[7])));
+}
+__device__ __forceinline__ void add_turn(uint32_t at, float (&v)[8])
+{
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        v[2 * k] += __uint_as_float(w[k] << 16);
+        v[2 * k + 1] += __uint_as_float(w[k] & 0xffff0000u);
+    }
 }
 // N sums of a row, from column `col` on; bias: of those columns.
 template <Epilogue EPI, int N>
@@ -147,17 +176,30 @@ __device__ __forceinline__ void finish(const Output& o, int row, int col, float 
 }
 
 // ---- pairs of SMs ----------------------------------------------------------------------------------------------------------
-constexpr int kPairWarps = 8, kPairThreads = 64 + 32 * kPairWarps;    // warp 0 copies, warp 1 issues, the others run the epilogue
+// Warp 0 copies, warp 1 issues, the others run the epilogue: sixteen where it has activations to compute, whose chains of dependent
+// instructions eight warps do not hide (128 columns each; 32768 x 512 -> 2048, SiLU, pre-activations kept: 113 us, now @@).
+template <Epilogue EPI> constexpr int kPairWarps = EPI == LAYER ? 16 : 8;
+template <Epilogue EPI> constexpr int kPairThreads = 64 + 32 * kPairWarps<EPI>;
 constexpr int kPairM = 256, kPairN = 256, kHalf = kPairN / 2;
 constexpr int kPairA = 128 * 128, kPairStage = kPairA + kHalf * 128;
 constexpr int kTurn = 32 * 128;                 // a warp's box of outputs on its way to memory: 32 rows x 64 columns
-template <Epilogue EPI> constexpr int kTurns = EPI == LAYER ? 2 : EPI == PLAIN ? 1 : 0;       // boxes of a warp
-template <Epilogue EPI> constexpr int kPairStages = 6 - kTurns<EPI>;
-template <Epilogue EPI> constexpr int kPairSmem = 1024 + kPairStages<EPI> * kPairStage + kPairWarps * kTurns<EPI> * kTurn;
+template <Epilogue EPI> constexpr int kPairStages = EPI == LAYER ? 5 : 6;
+// All of a block's shared memory is one piece, so that the stages start on a 1024-byte boundary without room to spare.
+template <Epilogue EPI> struct PairShared {
+    uint8_t stages[kPairStages<EPI>][kPairStage];
+    uint8_t turns[EPI == PLANES ? 1 : kPairWarps<EPI>][kTurn];
+    float bias[EPI == LAYER ? 2 : 1][kPairN];
+    uint64_t bars[2 * kPairStages<EPI> + 4 + kPairWarps<EPI>];
+    uint32_t tmem_slot;
+    int abort_flag;
+};
+static_assert(sizeof(PairShared<LAYER>) <= 227 * 1024 && sizeof(PairShared<PLAIN>) <= 227 * 1024 && sizeof(PairShared<PLANES>) <= 227 * 1024, "a block's shared memory");
 
 struct Work {
     int m_tiles, n_tiles, ranges;               // of k, each of `blocks` blocks (the last may have fewer)
     int blocks, all_blocks;
+    int box_rows;                               // of A's boxes on single SMs: 128, fewer where A has fewer (the rest of the tile is not used)
+    int plane_blocks, plane_rows;               // A's planes follow each other along k: blocks of one, rows between two
 };
 
 // One operand's tile of a block of k: `rows` M or N elements of this CTA from element `e0` on, k from k0.
@@ -175,38 +217,35 @@ __device__ __forceinline__ uint64_t tile_desc(uint32_t addr) { return ROWS ? sme
 template <bool ROWS> constexpr uint32_t kStepK = ROWS ? 2048 / 16 : 32 / 16;        // descriptor units per 16 of k
 
 template <bool A_ROWS, bool B_ROWS, Epilogue EPI>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads<EPI>)
 linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmY,
-                   const __grid_constant__ CUtensorMap tmPre, const Work wk, const Output o)
+                   const __grid_constant__ CUtensorMap tmPre, const __grid_constant__ CUtensorMap tmRes, const Work wk, const Output o)
 {
-    constexpr int NST = kPairStages<EPI>;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * NST + 4];
-    uint64_t *full_bar = bars, *empty_bar = bars + NST, *acc_full = empty_bar + NST, *acc_empty = acc_full + 2;
-    __shared__ uint32_t tmem_slot;
-    __shared__ int abort_flag;
-    __shared__ __align__(16) float s_bias[2][kPairN];
-    volatile int* abortp = &abort_flag;
+    constexpr int NST = kPairStages<EPI>, WARPS = kPairWarps<EPI>, COLS = kPairN / (WARPS / 4);
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    PairShared<EPI>& sh = *reinterpret_cast<PairShared<EPI>*>(smem_raw);
+    uint64_t *bars = sh.bars, *full_bar = bars, *empty_bar = bars + NST, *acc_full = empty_bar + NST, *acc_empty = acc_full + 2, *res_full = acc_empty + 2;
+    volatile int* abortp = &sh.abort_flag;
 
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;      // the same offset in both CTAs
+    const uint32_t base = smem_u32(smem_raw);           // the same offset in both CTAs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank();
     if (warp == 0) {
-        if (lane < 2 * NST + 4) mbar_init(&bars[lane], lane < 2 * NST + 2 ? 1 : 2 * kPairWarps);
+        if (lane < 2 * NST + 4 + WARPS) mbar_init(&bars[lane], lane >= 2 * NST + 2 && lane < 2 * NST + 4 ? 2 * WARPS : 1);
         fence_barrier_init();
     } else if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2 * kPairN) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_slot)), "r"(2 * kPairN) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     } else if (warp == 2 && lane == 0) {
-        abort_flag = 0;
+        sh.abort_flag = 0;
         tma_prefetch_desc(&tmA);
         tma_prefetch_desc(&tmB);
     }
-    static_assert(2 * NST + 4 <= 32, "a lane initialises one barrier");
+    static_assert(2 * NST + 4 + WARPS <= 32, "a lane initialises one barrier");
     tc_fence_before();
     cluster_sync();                                      // of both CTAs' threads: the partner's barriers exist
     tc_fence_after();
-    const uint32_t tmem_d = tmem_slot;
+    const uint32_t tmem_d = sh.tmem_slot;
     pdl_wait();
     pdl_trigger();
 
@@ -231,8 +270,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     if (it >= NST && !mbar_wait(&empty_bar[st], ((uint32_t)(it / NST) & 1u) ^ 1u, abortp, nullptr, 0)) { alive = false; break; }
                     const uint32_t dst = base + st * kPairStage, bar = in_cta(&full_bar[st], 0);
                     if (rank == 0) mbar_arrive_expect_tx(&full_bar[st], 2 * kPairStage);
-                    const int k = (k0 + b) * kBlockK;
-                    pair_load<A_ROWS>(dst, &tmA, m0 + rank * 128, k, bar);
+                    const int plane = (k0 + b) / wk.plane_blocks, k = (k0 + b - plane * wk.plane_blocks) * kBlockK, shift = plane * wk.plane_rows;
+                    pair_load<A_ROWS>(dst, &tmA, m0 + rank * 128 + (A_ROWS ? 0 : shift), k + (A_ROWS ? shift : 0), bar);
                     pair_load<B_ROWS>(dst + kPairA, &tmB, n0 + rank * kHalf, k, bar);
                 }
             }
@@ -264,80 +303,125 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         }
     } else {
         // epilogue warps: lane quarter warp % 4, a share of the tile's columns
-        constexpr int COLS = kPairN / (kPairWarps / 4);
         const int q = warp & 3, share = (warp - 2) >> 2, id = threadIdx.x - 64;
-        const uint32_t turn_smem = base + NST * kPairStage + (warp - 2) * kTurns<EPI> * kTurn;
+        const uint32_t turn_smem = base + NST * kPairStage + (EPI == PLANES ? 0 : warp - 2) * kTurn, to = turn_smem + lane * 128;
         int turn = 0;
         bool ok = true;
         auto bias_of = [&](int w) {             // this thread's column of a tile; asked for a tile ahead
             const int col = w % wk.n_tiles * kPairN + id;
             return EPI == LAYER && o.bias && w < work && id < kPairN && col < o.cols ? o.bias[col] : 0.f;
         };
+        // Boxes of 64 columns.  The residual of a box is copied to where its outputs will be, one box ahead.
+        const bool boxes = EPI != PLANES && o.vec >= 8, with_residual = EPI == LAYER && o.residual;
+        int box = 0;
+        auto residual_ahead = [&](int w, int c) {       // lane 0: the buffer is free
+            if (w >= work) return;
+            int m0, n0, range, k0, blocks;
+            item(w, m0, n0, range, k0, blocks);
+            mbar_arrive_expect_tx(&res_full[warp - 2], kTurn);
+            tma_load_2d(smem_raw + (turn_smem - smem_u32(smem_raw)), &tmRes, n0 + share * COLS + c, m0 + rank * 128 + q * 32, &res_full[warp - 2]);
+        };
+        if (boxes && with_residual && lane == 0) residual_ahead(blockIdx.x / 2, 0);
         float next_bias = bias_of(blockIdx.x / 2);
         for (int w = blockIdx.x / 2; w < work; w += pairs, ++turn) {
             int m0, n0, range, k0, blocks;
             item(w, m0, n0, range, k0, blocks);
             const int acc = turn & 1, row = m0 + rank * 128 + q * 32 + lane;
             if (EPI == LAYER && o.bias) {       // the buffer of two tiles ago: every warp has passed the barrier of the last
-                if (id < kPairN) s_bias[acc][id] = next_bias;
+                if (id < kPairN) sh.bias[EPI == LAYER ? acc : 0][id] = next_bias;
                 next_bias = bias_of(w + pairs);
-                asm volatile("bar.sync 1, %0;" ::"n"(32 * kPairWarps) : "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(32 * WARPS) : "memory");
             }
             ok = ok && mbar_wait_warp(&acc_full[acc], (uint32_t)(turn >> 1) & 1u, abortp, nullptr, 0);
             tc_fence_after();
             const uint32_t taddr = tmem_d + acc * kPairN + share * COLS + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1
             for (int c = 0; c < COLS; c += 64) {
-                uint32_t r[64];
-                tmem_ld_32x32(taddr + c, reinterpret_cast<uint32_t(&)[32]>(r[0]));
-                tmem_ld_32x32(taddr + c + 32, reinterpret_cast<uint32_t(&)[32]>(r[32]));
-                tmem_ld_wait();
-                if (c + 64 == COLS) {           // the accumulator is in registers: hand it back
+                const int cc = share * COLS + c, valid = o.cols - n0 - cc;
+                const float* bias = EPI == LAYER && o.bias ? &sh.bias[EPI == LAYER ? acc : 0][cc] : nullptr;
+                uint32_t r[32];
+                auto load = [&](int hf) {       // 32 sums of this thread's row
+                    tmem_ld_32x32(taddr + c + hf, r);
+                    tmem_ld_wait();
+                    if (!ok)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[i] = 0x7fffffff;
+                };
+                auto hand_back = [&] {          // the accumulator's last columns are in registers
+                    if (c + 64 != COLS) return;
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0 && w + 2 * pairs < work) arrive_cluster_relaxed(in_cta(&acc_empty[acc], 0));     // what is waited for, and no more
-                }
-                if (!ok)
+                };
+                auto sums = [&](int hf, int g, auto& v) {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) r[i] = 0x7fffffff;
-                const int cc = share * COLS + c, valid = o.cols - n0 - cc;
-                const float* bias = EPI == LAYER && o.bias ? &s_bias[acc][cc] : nullptr;
-                if (EPI != PLANES && o.vec >= 8) {
+                    for (int i = 0; i < (int)(sizeof(v) / 4); ++i) v[i] = __uint_as_float(r[g + i]) + (EPI == LAYER && bias ? bias[hf + g + i] : 0.f);
+                };
+                if (boxes) {
                     // rounded into a box in the copies' 128-byte swizzle, a row per lane, and from there to memory in whole lines
-                    if (lane == 0) tma_store_wait_read();
+                    if (with_residual) ok = ok && mbar_wait_warp(&res_full[warp - 2], box & 1, abortp, nullptr, 0);
+                    else if (lane == 0) tma_store_wait_read();
                     __syncwarp();
-#pragma unroll
-                    for (int g = 0; g < 8; ++g) {
-                        float v[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[8 * g + i]);
-                        const uint32_t at = turn_smem + lane * 128 + ((g ^ (lane & 7)) * 16);
-                        if (EPI == LAYER) {
-                            if (bias) {
-                                const float4 lo = *reinterpret_cast<const float4*>(bias + 8 * g), hi = *reinterpret_cast<const float4*>(bias + 8 * g + 4);
-                                v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w; v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
-                            }
-                            if (o.pre) store_turn(at + kTurn, v);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], o.activation);
-                            if (o.residual && row < o.rows && 8 * g < valid) add_row(o.residual + row * o.ld_res + n0 + cc + 8 * g, v, valid - 8 * g, o.vec);
+                    auto send = [&](const CUtensorMap* map) {
+                        fence_async_proxy();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (valid > 0) tma_store_2d(map, turn_smem, n0 + cc, row);
+                            tma_store_commit();
                         }
-                        store_turn(at, v);
+                    };
+                    const bool twice = EPI == LAYER && o.pre;
+#pragma unroll
+                    for (int hf = 0; hf < 64; hf += 32) {
+                        load(hf);
+                        if (hf && !twice) hand_back();
+#pragma unroll
+                        for (int g = 0; g < 32; g += 8) {
+                            float v[8];
+                            sums(hf, g, v);
+                            const uint32_t at = to + (((hf + g) / 8 ^ (lane & 7)) * 16);
+                            if (EPI == LAYER) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], o.activation);
+                                if (with_residual) add_turn(at, v);
+                            }
+                            store_turn(at, v);
+                        }
                     }
-                    fence_async_proxy();
-                    __syncwarp();
-                    if (lane == 0 && valid > 0) {
-                        tma_store_2d(&tmY, turn_smem, n0 + cc, row);
-                        if (EPI == LAYER && o.pre) tma_store_2d(&tmPre, turn_smem + kTurn, n0 + cc, row);
-                        tma_store_commit();
+                    send(&tmY);
+                    if (twice) {
+                        if (lane == 0) tma_store_wait_read();
+                        __syncwarp();
+#pragma unroll
+                        for (int hf = 0; hf < 64; hf += 32) {
+                            load(hf);
+                            if (hf) hand_back();
+#pragma unroll
+                            for (int g = 0; g < 32; g += 8) {
+                                float v[8];
+                                sums(hf, g, v);
+                                store_turn(to + (((hf + g) / 8 ^ (lane & 7)) * 16), v);
+                            }
+                        }
+                        send(&tmPre);
                     }
+                    if (with_residual && lane == 0) {
+                        tma_store_wait_read();
+                        if (c + 64 < COLS) residual_ahead(w, c + 64);
+                        else residual_ahead(w + pairs, 0);
+                    }
+                    ++box;
                 } else
 #pragma unroll
-                    for (int g = 0; g < 64; g += 16) {
-                        float v[16];
+                    for (int hf = 0; hf < 64; hf += 32) {
+                        load(hf);
+                        if (hf) hand_back();
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[g + i]);
-                        finish<EPI, 16>(o, row, n0 + cc + g, v, bias ? bias + g : nullptr, range);
+                        for (int g = 0; g < 32; g += 16) {
+                            float v[16];
+                            sums(hf, g, v);
+                            finish<EPI, 16>(o, row, n0 + cc + hf + g, v, nullptr, range);
+                        }
                     }
             }
         }
@@ -353,7 +437,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 
 // ---- clusters along k -------------------------------------------------------------------------------------------------------
 constexpr int kSplitThreads = 192;              // warp 0 copies, warp 1 issues, warps 2..5 empty the accumulator; then all run the epilogue
-constexpr int kSplitN = 64, kSplitStages = 4, kSplitA = 128 * 128, kSplitStage = kSplitA + kSplitN * 128;
+constexpr int kSplitN = 64, kSplitStages = 8, kSplitA = 128 * 128, kSplitStage = kSplitA + kSplitN * 128;
 constexpr int kPartialPitch = kSplitN + 4;      // floats: rows start four banks apart
 constexpr int kSplitSmem = 1024 + (kSplitStages * kSplitStage > 128 * kPartialPitch * 4 ? kSplitStages * kSplitStage : 128 * kPartialPitch * 4);
 
@@ -394,11 +478,11 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     if (warp == 0) {
         if (lane == 0)
             for (int b = 0; b < blocks; ++b) {
-                const int st = b % kSplitStages, k = (k0 + b) * kBlockK;
+                const int st = b % kSplitStages, at = k0 + (b + tile) % blocks, plane = at / wk.plane_blocks, k = (at - plane * wk.plane_blocks) * kBlockK;
                 if (b >= kSplitStages && !mbar_wait(&empty_bar[st], ((uint32_t)(b / kSplitStages) & 1u) ^ 1u, abortp, nullptr, 0)) break;
-                mbar_arrive_expect_tx(&full_bar[st], kSplitStage);
+                mbar_arrive_expect_tx(&full_bar[st], (wk.box_rows + kSplitN) * 128);
                 uint8_t* dst = reinterpret_cast<uint8_t*>(partial) + st * kSplitStage;
-                tma_load_2d(dst, &tmA, k, m0, &full_bar[st]);
+                tma_load_2d(dst, &tmA, k, m0 + plane * wk.plane_rows, &full_bar[st]);
                 if (B_ROWS) tma_load_2d(dst + kSplitA, &tmB, n0, k, &full_bar[st]);
                 else tma_load_2d(dst + kSplitA, &tmB, k, n0, &full_bar[st]);
             }
@@ -472,11 +556,12 @@ __global__ void __launch_bounds__(256) pack_kernel(const bf16* from, int64_t ld,
     }
 }
 
-// dz = dy act'(pre), rounded, and its sums over 64 rows: part[row block][cols].  V channels a thread.
+// dz = dy act'(pre), rounded (with `low`, what the rounding left out, rounded, in a second plane), and its sums over 64 rows:
+// part[row block][cols].  V channels a thread.
 constexpr int kSumRows = 64;
 template <int V>
 __global__ void __launch_bounds__(256) dz_kernel(const bf16* dy, int64_t ld_dy, const bf16* pre, int64_t ld_pre, int rows, int cols, int act, bf16* dz, int ld_dz,
-                                                 float* part)
+                                                 bool low, float* part)
 {
     pdl_wait();
     pdl_trigger();
@@ -499,7 +584,14 @@ __global__ void __launch_bounds__(256) dz_kernel(const bf16* dy, int64_t ld_dy, 
             }
 #pragma unroll
             for (int k = 0; k < V; ++k) sum[k] += v[k];
-            if (dz) store_vec<V>(dz + row * ld_dz + c, v);
+            if (dz) {
+                store_vec<V>(dz + row * ld_dz + c, v);
+                if (low) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) v[k] = fabsf(v[k]) < INFINITY ? v[k] - to_float(from_float<bf16>(v[k])) : 0.f;
+                    store_vec<V>(dz + (rows + row) * ld_dz + c, v);
+                }
+            }
         }
     if (!part) return;
 #pragma unroll
@@ -532,35 +624,37 @@ __global__ void __launch_bounds__(256) planes_kernel(const float* planes, int co
 int padded(int cols) { return (cols + 7) / 8 * 8; }
 bool as_is(const void* p, int64_t ld) { return aligned_to(p, 16) && ld % 8 == 0; }
 
-struct Operand { const bf16* p; int64_t ld; };
+struct Operand { const bf16* p; int64_t ld; int planes = 1; };
 // The operand itself, or a copy of it where its rows do not start on 16-byte boundaries.
 hts_status laid_out(const bf16* p, int64_t ld, int rows, int cols, bf16* copy, Operand* out, cudaStream_t s)
 {
-    *out = {p, ld};
+    *out = Operand{p, ld};
     if (as_is(p, ld)) return HTS_OK;
     const int64_t blocks = ceil_div((int64_t)rows * padded(cols), 1024);
     HTS_CUDA(launch_pdl(pack_kernel, dim3((unsigned)(blocks < 16 * kCoreSms ? blocks : 16 * kCoreSms)), dim3(256), 0, s, p, ld, (int64_t)rows, cols, padded(cols), copy));
     note_launch();
-    *out = {copy, padded(cols)};
+    *out = Operand{copy, padded(cols)};
     return HTS_OK;
 }
 
 template <bool A_ROWS, bool B_ROWS, Epilogue EPI>
 hts_status launch_pairs(const Operand& a, const Operand& b, int M, int N, int K, int ranges, const Output& o, cudaStream_t s)
 {
-    CUtensorMap ma, mb, my{}, mp{};
+    CUtensorMap ma, mb, my{}, mp{}, mr{};
     if (EPI != PLANES && o.vec >= 8 &&
-        (!make_bf16_map(&my, o.y, M, N, o.ld_y, 32) || (o.pre && !make_bf16_map(&mp, o.pre, M, N, o.ld_pre, 32))))
+        (!make_bf16_map(&my, o.y, M, N, o.ld_y, 32) || (o.pre && !make_bf16_map(&mp, o.pre, M, N, o.ld_pre, 32)) ||
+         (o.residual && !make_bf16_map(&mr, o.residual, M, N, o.ld_res, 32))))
         return HTS_ERR_CUDA;
-    if (!(A_ROWS ? make_bf16_map(&ma, a.p, K, M, a.ld, 64) : make_bf16_map(&ma, a.p, M, K, a.ld, 128)) ||
+    if (!(A_ROWS ? make_bf16_map(&ma, a.p, (uint64_t)a.planes * K, M, a.ld, 64) : make_bf16_map(&ma, a.p, (uint64_t)a.planes * M, K, a.ld, 128)) ||
         !(B_ROWS ? make_bf16_map(&mb, b.p, K, N, b.ld, 64) : make_bf16_map(&mb, b.p, N, K, b.ld, kHalf)))
         return HTS_ERR_CUDA;
-    Work w{(int)ceil_div(M, kPairM), (int)ceil_div(N, kPairN), ranges, 0, (int)ceil_div(K, kBlockK)};
+    const int plane_blocks = (int)ceil_div(K, kBlockK);
+    Work w{(int)ceil_div(M, kPairM), (int)ceil_div(N, kPairN), ranges, 0, a.planes * plane_blocks, 128, plane_blocks, A_ROWS ? K : M};
     w.blocks = (int)ceil_div(w.all_blocks, ranges);
     static OncePerDevice allowed;
     HTS_CUDA(allow_shared(linear_pair_kernel<A_ROWS, B_ROWS, EPI>, allowed));
     const int64_t work = (int64_t)w.m_tiles * w.n_tiles * ranges, pairs = device_sm_count(device_slot()) / 2;
-    HTS_CUDA(launch_pdl(linear_pair_kernel<A_ROWS, B_ROWS, EPI>, dim3((unsigned)(2 * (work < pairs ? work : pairs))), dim3(kPairThreads), (size_t)kPairSmem<EPI>, s, ma, mb, my, mp, w, o));
+    HTS_CUDA(launch_pdl(linear_pair_kernel<A_ROWS, B_ROWS, EPI>, dim3((unsigned)(2 * (work < pairs ? work : pairs))), dim3(kPairThreads<EPI>), sizeof(PairShared<EPI>), s, ma, mb, my, mp, mr, w, o));
     note_launch();
     return HTS_OK;
 }
@@ -568,8 +662,10 @@ template <bool B_ROWS, Epilogue EPI>
 hts_status launch_split(const Operand& a, const Operand& b, int M, int N, int K, const Output& o, cudaStream_t s)
 {
     CUtensorMap ma, mb;
-    if (!make_bf16_map(&ma, a.p, M, K, a.ld, 128) || !(B_ROWS ? make_bf16_map(&mb, b.p, K, N, b.ld, 64) : make_bf16_map(&mb, b.p, N, K, b.ld, kSplitN))) return HTS_ERR_CUDA;
-    Work w{(int)ceil_div(M, 128), (int)ceil_div(N, kSplitN), 1, 0, (int)ceil_div(K, kBlockK)};
+    const int box_rows = M < 128 ? (M + 7) / 8 * 8 : 128;
+    if (!make_bf16_map(&ma, a.p, (uint64_t)a.planes * M, K, a.ld, box_rows) || !(B_ROWS ? make_bf16_map(&mb, b.p, K, N, b.ld, 64) : make_bf16_map(&mb, b.p, N, K, b.ld, kSplitN))) return HTS_ERR_CUDA;
+    const int plane_blocks = (int)ceil_div(K, kBlockK);
+    Work w{(int)ceil_div(M, 128), (int)ceil_div(N, kSplitN), 1, 0, a.planes * plane_blocks, box_rows, plane_blocks, M};
     const int64_t tiles = (int64_t)w.m_tiles * w.n_tiles;
     int ranks = 8;
     while (ranks > 1 && (tiles * ranks > kCoreSms || ranks > w.all_blocks)) ranks /= 2;
@@ -589,11 +685,12 @@ hts_status launch_split(const Operand& a, const Operand& b, int M, int N, int K,
     note_launch();
     return HTS_OK;
 }
-// Pairs of SMs where their 256 x 256 tiles keep half of the device busy, else 128 x 64 tiles cut along k.
+// Pairs of SMs from ten 256 x 256 tiles on, else 128 x 64 tiles cut along k: both take 12.5 us for 1024 x 1024 -> 2048 (32 tiles), 256 x 1024 -> 2048
+// (8 tiles) takes 9.5 us cut and 12.3 in pairs, 4096 x 512 -> 512 (32) 10.3 and 8.6.
 template <bool B_ROWS, Epilogue EPI>
 hts_status launch_product(const Operand& a, const Operand& b, int M, int N, int K, const Output& o, cudaStream_t s)
 {
-    if (ceil_div(M, kPairM) * ceil_div(N, kPairN) * 4 >= kCoreSms) return launch_pairs<false, B_ROWS, EPI>(a, b, M, N, K, 1, o, s);
+    if (ceil_div(M, kPairM) * ceil_div(N, kPairN) * 16 >= kCoreSms) return launch_pairs<false, B_ROWS, EPI>(a, b, M, N, K, 1, o, s);
     return launch_split<B_ROWS, EPI>(a, b, M, N, K, o, s);
 }
 
@@ -606,14 +703,17 @@ int vec_of(std::initializer_list<const void*> pointers, std::initializer_list<in
 }
 
 // Ranges of dw's long k: enough for every pair of SMs, eight blocks of k each at least.
-int dw_ranges(int M, int K, int N)
+int dw_ranges(int M, int K, int N, int planes)
 {
-    const int64_t tiles = ceil_div(N, kPairM) * ceil_div(K, kPairN), blocks = ceil_div(M, kBlockK);
+    const int64_t tiles = ceil_div(N, kPairM) * ceil_div(K, kPairN), blocks = planes * ceil_div(M, kBlockK);
     int64_t r = kCoreSms / 2 / tiles;
     if (r > blocks / 8) r = blocks / 8;
     if (r < 1) r = 1;
     return (int)ceil_div(blocks, ceil_div(blocks, r));           // no range is empty
 }
+// dz has an error of its own, up to 2^-8 of each element.  In long sums it stays below the outputs' rounding; with few elements it need
+// not, and there a second plane with what was left out costs next to nothing: the products take a few us for any K.
+int dz_planes(int M, int N) { return (int64_t)M * N <= 1 << 18 ? 2 : 1; }
 struct LinearPlan { size_t x, w, dz, sums, planes, bytes; int ranges; };
 LinearPlan linear_plan(int M, int K, int N, bool gradient)
 {
@@ -623,8 +723,8 @@ LinearPlan linear_plan(int M, int K, int N, bool gradient)
     q.x = take((size_t)M * padded(K) * 2);
     q.w = take((size_t)N * padded(K) * 2);
     if (gradient) {
-        q.ranges = dw_ranges(M, K, N);
-        q.dz = take((size_t)M * padded(N) * 2);
+        q.ranges = dw_ranges(M, K, N, dz_planes(M, N));
+        q.dz = take((size_t)dz_planes(M, N) * M * padded(N) * 2);
         q.sums = take((size_t)ceil_div(M, kSumRows) * N * 4);
         q.planes = take((size_t)q.ranges * N * K * 4);
     }
@@ -693,9 +793,9 @@ extern "C" hts_status hts_linear_gradient(const hts_linear_desc* d, const void* 
         const int64_t blocks = ceil_div(M, kSumRows) * ceil_div(N, wide ? 256 : 32);
         if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
         HTS_CUDA(launch_pdl(wide ? dz_kernel<8> : dz_kernel<1>, dim3((unsigned)blocks), dim3(32, 8), 0, s, (const bf16*)dy, d->ld_dy, (const bf16*)pre, d->ld_pre, M, N,
-                            d->activation, dz, padded(N), part));
+                            d->activation, dz, padded(N), act && dz_planes(M, N) > 1, part));
         note_launch();
-        if (dz) g = {dz, padded(N)};
+        if (dz) g = Operand{dz, padded(N), act ? dz_planes(M, N) : 1};
         if (dbias) {
             const hts_status st = launch_column_sums({part, ceil_div(M, kSumRows), N, N, N, 1, dbias, nullptr, N, nullptr}, s);
             if (st != HTS_OK) return st;
@@ -714,12 +814,13 @@ extern "C" hts_status hts_linear_gradient(const hts_linear_desc* d, const void* 
         if (st != HTS_OK) return st;
         Output o{};
         o.rows = N; o.cols = K; o.planes = (float*)(ws + q.planes); o.vec = K % 4 == 0 ? 8 : 1;
-        st = launch_pairs<true, true, PLANES>(g, a, N, K, M, q.ranges, o, s);
+        const int ranges = dw_ranges(M, K, N, g.planes);                // no more than the workspace has room for
+        st = launch_pairs<true, true, PLANES>(g, a, N, K, M, ranges, o, s);
         if (st != HTS_OK) return st;
         const int64_t size = (int64_t)N * K;
         const dim3 grid((unsigned)ceil_div(size, 256));
-        if (d->dw_dtype == HTS_DTYPE_FP32) HTS_CUDA(launch_pdl(planes_kernel<float>, grid, dim3(256), 0, s, (const float*)o.planes, q.ranges, size, (float*)dw));
-        else HTS_CUDA(launch_pdl(planes_kernel<bf16>, grid, dim3(256), 0, s, (const float*)o.planes, q.ranges, size, (bf16*)dw));
+        if (d->dw_dtype == HTS_DTYPE_FP32) HTS_CUDA(launch_pdl(planes_kernel<float>, grid, dim3(256), 0, s, (const float*)o.planes, ranges, size, (float*)dw));
+        else HTS_CUDA(launch_pdl(planes_kernel<bf16>, grid, dim3(256), 0, s, (const float*)o.planes, ranges, size, (bf16*)dw));
         note_launch();
     }
     return HTS_OK;
