@@ -177,7 +177,7 @@ __device__ __forceinline__ void finish(const Output& o, int row, int col, float 
 
 // ---- pairs of SMs ----------------------------------------------------------------------------------------------------------
 // Warp 0 copies, warp 1 issues, the others run the epilogue: sixteen where it has activations to compute, whose chains of dependent
-// instructions eight warps do not hide (128 columns each; 32768 x 512 -> 2048, SiLU, pre-activations kept: 113 us, now @@).
+// instructions eight warps do not hide (128 columns each; 32768 x 512 -> 2048, SiLU, pre-activations kept: 113 us, now 96).
 template <Epilogue EPI> constexpr int kPairWarps = EPI == LAYER ? 16 : 8;
 template <Epilogue EPI> constexpr int kPairThreads = 64 + 32 * kPairWarps<EPI>;
 constexpr int kPairM = 256, kPairN = 256, kHalf = kPairN / 2;
@@ -437,14 +437,19 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 
 // ---- clusters along k -------------------------------------------------------------------------------------------------------
 constexpr int kSplitThreads = 192;              // warp 0 copies, warp 1 issues, warps 2..5 empty the accumulator; then all run the epilogue
-constexpr int kSplitN = 64, kSplitStages = 8, kSplitA = 128 * 128, kSplitStage = kSplitA + kSplitN * 128;
-constexpr int kPartialPitch = kSplitN + 4;      // floats: rows start four banks apart
-constexpr int kSplitSmem = 1024 + (kSplitStages * kSplitStage > 128 * kPartialPitch * 4 ? kSplitStages * kSplitStage : 128 * kPartialPitch * 4);
+constexpr int kSplitA = 128 * 128;
+template <int SN> struct SplitShape {           // 128 x SN outputs
+    static constexpr int kStage = kSplitA + SN * 128, kStages = SN == 64 ? 8 : 6;
+    static constexpr int kPitch = SN + 4;       // floats: rows of partial sums start four banks apart
+    static constexpr int kSmem = 1024 + (kStages * kStage > 128 * kPitch * 4 ? kStages * kStage : 128 * kPitch * 4);
+};
 
-template <bool B_ROWS, Epilogue EPI>
+template <int SN, bool B_ROWS, Epilogue EPI>
 __global__ void __launch_bounds__(kSplitThreads)
 linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Work wk, const Output o)
 {
+    using S = SplitShape<SN>;
+    constexpr int kSplitStages = S::kStages, kSplitStage = S::kStage, kPartialPitch = S::kPitch;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_bar[kSplitStages], empty_bar[kSplitStages], done_bar;
     __shared__ uint32_t tmem_slot;
@@ -454,7 +459,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     float* partial = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank(), ranks = (int)cluster_size();
-    const int tile = blockIdx.x / ranks, n0 = tile % wk.n_tiles * kSplitN, m0 = tile / wk.n_tiles * 128;
+    const int tile = blockIdx.x / ranks, n0 = tile % wk.n_tiles * SN, m0 = tile / wk.n_tiles * 128;
     const int k0 = rank * wk.blocks, blocks = max(0, min(wk.blocks, wk.all_blocks - k0));
 
     if (warp == 0) {
@@ -462,7 +467,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         if (lane == 0) mbar_init(&done_bar, 1);
         fence_barrier_init();
     } else if (warp == 1)
-        tmem_alloc(&tmem_slot, kSplitN);
+        tmem_alloc(&tmem_slot, SN);
     else if (warp == 2 && lane == 0) {
         abort_flag = 0;
         tma_prefetch_desc(&tmA);
@@ -478,17 +483,19 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     if (warp == 0) {
         if (lane == 0)
             for (int b = 0; b < blocks; ++b) {
-                const int st = b % kSplitStages, at = k0 + (b + tile) % blocks, plane = at / wk.plane_blocks, k = (at - plane * wk.plane_blocks) * kBlockK;
+                const int st = b % kSplitStages, at = k0 + b, plane = at / wk.plane_blocks, k = (at - plane * wk.plane_blocks) * kBlockK;
                 if (b >= kSplitStages && !mbar_wait(&empty_bar[st], ((uint32_t)(b / kSplitStages) & 1u) ^ 1u, abortp, nullptr, 0)) break;
-                mbar_arrive_expect_tx(&full_bar[st], (wk.box_rows + kSplitN) * 128);
+                mbar_arrive_expect_tx(&full_bar[st], (wk.box_rows + SN) * 128);
                 uint8_t* dst = reinterpret_cast<uint8_t*>(partial) + st * kSplitStage;
                 tma_load_2d(dst, &tmA, k, m0 + plane * wk.plane_rows, &full_bar[st]);
-                if (B_ROWS) tma_load_2d(dst + kSplitA, &tmB, n0, k, &full_bar[st]);
+                if (B_ROWS)
+#pragma unroll
+                    for (int i = 0; i < SN; i += 64) tma_load_2d(dst + kSplitA + i * 128, &tmB, n0 + i, k, &full_bar[st]);
                 else tma_load_2d(dst + kSplitA, &tmB, k, n0, &full_bar[st]);
             }
     } else if (warp == 1) {
         if (elect_one()) {
-            constexpr uint32_t idesc = instr_desc_f16(1, 128, kSplitN) | ((uint32_t)B_ROWS << 16);
+            constexpr uint32_t idesc = instr_desc_f16(1, 128, SN) | ((uint32_t)B_ROWS << 16);
             bool alive = true;
             for (int b = 0; alive && b < blocks; ++b) {
                 const int st = b % kSplitStages;
@@ -508,7 +515,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
         tc_fence_after();
         if (!ok) let_copies_land();             // the partial sums' memory is the copies'
 #pragma unroll
-        for (int c = 0; c < kSplitN; c += 32) {
+        for (int c = 0; c < SN; c += 32) {
             uint32_t r[32];
             tmem_ld_32x32(tmem_d + c + ((uint32_t)(q * 32) << 16), r);
             tmem_ld_wait();
@@ -527,21 +534,30 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     cluster_sync();
     // eight columns of a row to a thread, the cluster's partial sums in rank order
     const int rows = min(128, o.rows - m0);
-    for (int e = rank * kSplitThreads + threadIdx.x; e < rows * (kSplitN / 8); e += ranks * kSplitThreads) {
-        const int row = e / (kSplitN / 8), c = e % (kSplitN / 8) * 8;
+    for (int e = rank * kSplitThreads + threadIdx.x; e < rows * (SN / 8); e += ranks * kSplitThreads) {
+        const int row = e / (SN / 8), c = e % (SN / 8) * 8;
         float v[8] = {}, bias[8];
-        for (int i = 0; i < ranks; ++i) {
-            const uint32_t at = in_cta(partial + row * kPartialPitch + c, i);
-            const float4 lo = load_cluster(at), hi = load_cluster(at + 16);
-            v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w; v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
-        }
+        float4 part[8][2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)             // all of them under way before the first is added
+            if (i < ranks) {
+                const uint32_t at = in_cta(partial + row * kPartialPitch + c, i);
+                part[i][0] = load_cluster(at);
+                part[i][1] = load_cluster(at + 16);
+            }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < ranks) {
+                v[0] += part[i][0].x; v[1] += part[i][0].y; v[2] += part[i][0].z; v[3] += part[i][0].w;
+                v[4] += part[i][1].x; v[5] += part[i][1].y; v[6] += part[i][1].z; v[7] += part[i][1].w;
+            }
         if (EPI == LAYER && o.bias)
 #pragma unroll
             for (int i = 0; i < 8; ++i) bias[i] = n0 + c + i < o.cols ? o.bias[n0 + c + i] : 0.f;
         finish<EPI, 8>(o, m0 + row, n0 + c, v, EPI == LAYER && o.bias ? bias : nullptr, 0);
     }
     cluster_sync();                             // nobody leaves while its sums are read
-    if (warp == 1) tmem_dealloc(tmem_d, kSplitN);
+    if (warp == 1) tmem_dealloc(tmem_d, SN);
 }
 
 // ---- around the products ----------------------------------------------------------------------------------------------------
@@ -658,23 +674,31 @@ hts_status launch_pairs(const Operand& a, const Operand& b, int M, int N, int K,
     note_launch();
     return HTS_OK;
 }
-template <bool B_ROWS, Epilogue EPI>
+// Ranks of a cluster for `tiles` tiles and `blocks` blocks of k.  A block has its SM alone, and clusters lie within a group of 16 to 20
+// SMs: sixteen clusters of eight do not run at once (128 x 1024 -> 2048 in 128 x 128 tiles takes 20 us, in clusters of four 9.7).
+int split_ranks(int64_t tiles, int blocks)
+{
+    int ranks = tiles <= 8 ? 8 : tiles <= 32 ? 4 : tiles <= kCoreSms / 2 ? 2 : 1;
+    while (ranks > blocks) ranks /= 2;
+    return ranks;
+}
+template <int SN, bool B_ROWS, Epilogue EPI>
 hts_status launch_split(const Operand& a, const Operand& b, int M, int N, int K, const Output& o, cudaStream_t s)
 {
     CUtensorMap ma, mb;
     const int box_rows = M < 128 ? (M + 7) / 8 * 8 : 128;
-    if (!make_bf16_map(&ma, a.p, (uint64_t)a.planes * M, K, a.ld, box_rows) || !(B_ROWS ? make_bf16_map(&mb, b.p, K, N, b.ld, 64) : make_bf16_map(&mb, b.p, N, K, b.ld, kSplitN))) return HTS_ERR_CUDA;
+    if (!make_bf16_map(&ma, a.p, (uint64_t)a.planes * M, K, a.ld, box_rows) || !(B_ROWS ? make_bf16_map(&mb, b.p, K, N, b.ld, 64) : make_bf16_map(&mb, b.p, N, K, b.ld, SN)))
+        return HTS_ERR_CUDA;
     const int plane_blocks = (int)ceil_div(K, kBlockK);
-    Work w{(int)ceil_div(M, 128), (int)ceil_div(N, kSplitN), 1, 0, a.planes * plane_blocks, box_rows, plane_blocks, M};
+    Work w{(int)ceil_div(M, 128), (int)ceil_div(N, SN), 1, 0, a.planes * plane_blocks, box_rows, plane_blocks, M};
     const int64_t tiles = (int64_t)w.m_tiles * w.n_tiles;
-    int ranks = 8;
-    while (ranks > 1 && (tiles * ranks > kCoreSms || ranks > w.all_blocks)) ranks /= 2;
+    const int ranks = split_ranks(tiles, w.all_blocks);
     w.blocks = (int)ceil_div(w.all_blocks, ranks);
     static OncePerDevice allowed;
-    auto kernel = linear_split_kernel<B_ROWS, EPI>;
+    auto kernel = linear_split_kernel<SN, B_ROWS, EPI>;
     HTS_CUDA(allow_shared(kernel, allowed));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * ranks)); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = kSplitSmem; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)(tiles * ranks)); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = SplitShape<SN>::kSmem; cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -685,13 +709,25 @@ hts_status launch_split(const Operand& a, const Operand& b, int M, int N, int K,
     note_launch();
     return HTS_OK;
 }
-// Pairs of SMs from ten 256 x 256 tiles on, else 128 x 64 tiles cut along k: both take 12.5 us for 1024 x 1024 -> 2048 (32 tiles), 256 x 1024 -> 2048
-// (8 tiles) takes 9.5 us cut and 12.3 in pairs, 4096 x 512 -> 512 (32) 10.3 and 8.6.
+// What bounds a product of few tiles is the copies into each SM: rows and columns of its blocks of k, one tile after the other, and about
+// what 1500 of them take to begin and to end (measured: 2 us).  The least of three: tiles of 128 x 64, of 128 x 128, and pairs
+// (256 rows and columns each).  Against always taking one of them, us: 16 x 1024 -> 512 6.2 (64: 6.2, 128: 6.5), 64 x 4096 -> 4096 12.7 (64:
+// 16.2, pairs: 27), 256 x 1024 -> 2048 9.1 (128: 10.6, pairs: 12.3), 1024 x 4096 -> 512 14.4 (64: 17), 4096 x 512 -> 512 8.6 (64: 10.3),
+// 32768 x 512 -> 64 11.7 (64: 16.9).
+int64_t split_cost(int M, int N, int blocks, int SN)
+{
+    const int64_t tiles = ceil_div(M, 128) * ceil_div(N, SN);
+    const int ranks = split_ranks(tiles, blocks);
+    return ceil_div(tiles * ranks, kCoreSms) * (ceil_div(blocks, ranks) * (128 + SN) + 1500);
+}
 template <bool B_ROWS, Epilogue EPI>
 hts_status launch_product(const Operand& a, const Operand& b, int M, int N, int K, const Output& o, cudaStream_t s)
 {
-    if (ceil_div(M, kPairM) * ceil_div(N, kPairN) * 16 >= kCoreSms) return launch_pairs<false, B_ROWS, EPI>(a, b, M, N, K, 1, o, s);
-    return launch_split<B_ROWS, EPI>(a, b, M, N, K, o, s);
+    const int blocks = a.planes * (int)ceil_div(K, kBlockK);
+    const int64_t narrow = split_cost(M, N, blocks, 64), wide = split_cost(M, N, blocks, 128);
+    const int64_t pairs = ceil_div(ceil_div(M, kPairM) * ceil_div(N, kPairN), kCoreSms / 2) * blocks * 256 + 1500;
+    if (pairs <= narrow && pairs <= wide) return launch_pairs<false, B_ROWS, EPI>(a, b, M, N, K, 1, o, s);
+    return narrow <= wide ? launch_split<64, B_ROWS, EPI>(a, b, M, N, K, o, s) : launch_split<128, B_ROWS, EPI>(a, b, M, N, K, o, s);
 }
 
 int vec_of(std::initializer_list<const void*> pointers, std::initializer_list<int64_t> strides)
@@ -734,8 +770,8 @@ LinearPlan linear_plan(int M, int K, int N, bool gradient)
 bool bad(const hts_linear_desc* d)
 {
     return !d || d->rows < 1 || d->in_features < 1 || d->out_features < 1 || d->activation < HTS_ACT_NONE || d->activation > HTS_ACT_GELU ||
-           d->ld_x < d->in_features || ceil_div(d->rows, 128) * ceil_div(d->out_features, kSplitN) > INT32_MAX / 8 ||
-           ceil_div(d->rows, 128) * ceil_div(d->in_features, kSplitN) > INT32_MAX / 8 || (int64_t)d->out_features * d->in_features > ((int64_t)1 << 38);
+           d->ld_x < d->in_features || ceil_div(d->rows, 128) * ceil_div(d->out_features, 64) > INT32_MAX / 8 ||
+           ceil_div(d->rows, 128) * ceil_div(d->in_features, 64) > INT32_MAX / 8 || (int64_t)d->out_features * d->in_features > ((int64_t)1 << 38);
 }
 
 }  // namespace
