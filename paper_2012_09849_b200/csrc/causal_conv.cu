@@ -13,7 +13,7 @@ namespace hts {
 namespace {
 
 constexpr int kVector = 4, kGradVector = 2;     // channels of a thread where alignment allows, else one
-constexpr int kWarps = 8, kGroup = 4;           // warps of a block (a run each); steps loaded at once
+constexpr int kWarps = 8, kGroup = 4, kAhead = 3;      // warps of a block (a run each); steps of a group, groups asked for ahead
 
 struct ConvArgs {
     int T, N, D, lanes, runs, length;           // lanes: vectors of channels; runs per sequence, of `length` steps
@@ -101,42 +101,139 @@ __device__ __forceinline__ void weights(const ConvArgs& p, int c, float (&w)[W][
     }
 }
 
+// The inputs of a thread's run on their way to memory of its own, kAhead groups of steps before they are used: what a thread waits for
+// needs no registers, and no other thread.
+template <typename T, int V, int TENSORS>
+struct Feed {
+    Vec<T, V>* slots;                           // [tensor][kAhead + 1 groups][kGroup][threads]
+    const T* at[TENSORS];
+    int64_t step[TENSORS];
+    int left, slot;                             // steps that have not been asked for; where the next group goes
+    static constexpr int kSlots = (kAhead + 1) * kGroup, kThreads = 32 * kWarps;
+    __device__ __forceinline__ void ask()
+    {
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+#pragma unroll
+            for (int k = 0; k < TENSORS; ++k) {
+                if (j < left) copy_vec<V>(&slots[(k * kSlots + slot * kGroup + j) * kThreads], at[k]);
+                at[k] += step[k];
+            }
+        }
+        left -= kGroup;
+        slot = slot == kAhead ? 0 : slot + 1;
+        copies_commit();
+    }
+    // `steps` steps from the places in `at` on
+    __device__ __forceinline__ void begin(Vec<T, V>* own, int steps)
+    {
+        slots = own; left = steps; slot = 0;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) ask();
+    }
+    // the next group
+    __device__ __forceinline__ void take(float (&v)[TENSORS][kGroup][V])
+    {
+        copies_wait<kAhead - 1>();
+        const int now = slot == kAhead ? 0 : slot + 1;              // kAhead groups have been asked for since
+#pragma unroll
+        for (int k = 0; k < TENSORS; ++k)
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) {
+                const Vec<T, V> r = slots[(k * kSlots + now * kGroup + j) * kThreads];
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[k][j][i] = to_float(r.v[i]);
+            }
+        ask();
+    }
+};
+template <typename T, int V, int TENSORS> constexpr size_t kFeedBytes = TENSORS * Feed<T, V, TENSORS>::kSlots * Feed<T, V, TENSORS>::kThreads * sizeof(Vec<T, V>);
+
+// Which steps of the warp's sequence begin an episode, a bit each from the next step on; 32 are asked for at once, 32 ahead.
+struct Starts {
+    uint32_t bits = 0;
+    uint8_t ahead;
+    int have = 0, next;
+    __device__ __forceinline__ uint8_t load(const ConvArgs& p, int n, int t, int end) const
+    {
+        const int at = t + (int)threadIdx.x;
+        return p.starts && at < end ? p.starts[(size_t)at * p.N + n] : 0;
+    }
+    __device__ __forceinline__ void begin(const ConvArgs& p, int n, int t, int end) { ahead = load(p, n, t, end); next = t + 32; }
+    __device__ __forceinline__ uint32_t take(const ConvArgs& p, int n, int end)
+    {
+        if (!have) {
+            bits = __ballot_sync(0xffffffffu, ahead != 0);
+            ahead = load(p, n, next, end);
+            next += 32;
+            have = 32;
+        }
+        const uint32_t r = bits & ((1u << kGroup) - 1);
+        bits >>= kGroup;
+        have -= kGroup;
+        return r;
+    }
+};
+
+// The steps of a run in groups; a group without an episode start is one piece of code without a branch or a move between its steps.
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(32 * kWarps, 4) conv_kernel(const ConvArgs p, const T* x, const T* window_in, T* y, T* window_out)
+__global__ void __launch_bounds__(32 * kWarps, 3) conv_kernel(const ConvArgs p, const T* x, const T* window_in, T* y, T* window_out)
 {
+    extern __shared__ __align__(16) uint8_t s_mem[];
     pdl_wait();
     pdl_trigger();
     const Place q = place<V>(p);
-    if (!q.on) return;
+    if (!__any_sync(0xffffffffu, q.on)) return;
+    const int n = __reduce_max_sync(0xffffffffu, q.n), t0 = __reduce_max_sync(0xffffffffu, q.t0), stop = __reduce_max_sync(0xffffffffu, q.on ? q.t1 : 0);
+    Feed<T, V, 1> feed;
+    feed.at[0] = x + ((int64_t)t0 * p.N + n) * p.ld_x + q.c;
+    feed.step[0] = (int64_t)p.N * p.ld_x;
+    feed.begin(reinterpret_cast<Vec<T, V>*>(s_mem) + threadIdx.y * 32 + threadIdx.x, q.on ? stop - t0 : 0);
+    Starts starts;
+    starts.begin(p, n, t0, stop);
+    const int64_t step_y = (int64_t)p.N * p.ld_y;
+    T* to = y + ((int64_t)t0 * p.N + n) * p.ld_y + q.c;
     float w[W][V], b[V], win[W][V];
     weights(p, q.c, w, b);
     if (q.t0 < q.end || q.last) enter<T, V, W>(p, q, x, window_in, win);
-    for (int t = q.t0; t < q.t1; t += kGroup) {
-        Vec<T, V> raw[kGroup];
-        uint8_t st[kGroup];
+    for (int t = t0; t < stop; t += kGroup) {
+        float in[1][kGroup][V], v[kGroup + W - 1][V];       // the last inputs and the group's
+        feed.take(in);
+        const uint32_t fresh = starts.take(p, n, stop);
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
-            const size_t row = (size_t)min(t + j, q.t1 - 1) * p.N + q.n;
-            raw[j] = load_vec<V>(x + row * p.ld_x + q.c);
-            st[j] = p.starts ? p.starts[row] : 0;
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+            for (int k = 0; k < W - 1; ++k) v[k][i] = win[k + 1][i];
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) v[W - 1 + j][i] = in[0][j][i];
         }
+        auto output = [&](auto tap) {
+            float r[V];
 #pragma unroll
-        for (int j = 0; j < kGroup; ++j)
-            if (t + j < q.t1) {
-                float v[V];
+            for (int i = 0; i < V; ++i) {
+                float a = b[i];
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = to_float(raw[j].v[i]);
-                if (st[j]) clear(win);
-                push(win, v);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float a = b[i];
-#pragma unroll
-                    for (int k = 0; k < W; ++k) a = fmaf(w[k][i], win[k][i], a);
-                    v[i] = p.silu ? silu(a) : a;
-                }
-                store_vec<V>(y + ((size_t)(t + j) * p.N + q.n) * p.ld_y + q.c, v);
+                for (int k = 0; k < W; ++k) a = fmaf(w[k][i], tap(k, i), a);
+                r[i] = p.silu ? silu(a) : a;
             }
+            if (q.on) store_vec<V>(to, r);
+            to += step_y;
+        };
+        if (!fresh && t + kGroup <= stop) {
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) output([&](int k, int i) { return v[j + k][i]; });
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int k = 1; k < W; ++k) win[k][i] = v[kGroup - 1 + k][i];
+        } else
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j)
+                if (t + j < stop) {
+                    if (fresh >> j & 1) clear(win);
+                    push(win, v[W - 1 + j]);
+                    output([&](int k, int i) { return win[k][i]; });
+                }
     }
     if (q.last && window_out) {
 #pragma unroll
@@ -176,86 +273,144 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const ConvArgs p, const 
     for (int j = 0; j < W - 1; ++j) store_vec<V>(window_out + ((size_t)slot * (W - 1) + j) * p.D + c, win[j + 1]);
 }
 
-// A run walks W - 1 steps past its end, for the terms that those steps add to its inputs' gradients.  `pend[j]`: the gradient
-// of the input W - 1 - j steps back, complete when it reaches j = 0.  part: [block of runs][W + 1][D], weights then bias.
+// dx[u] = sum over i < W of w[W - 1 - i] g[u + i], g = dy act'(pre), up to the next start: it is formed when g[u + W - 1] is known, so
+// that a run walks W - 1 steps past its end.  part: [block of runs][W + 1][D], weights then bias.
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(32 * kWarps, 4) conv_gradient_kernel(const ConvArgs p, const T* x, const T* window_in, const T* dy, const float* dwindow_out,
+__global__ void __launch_bounds__(32 * kWarps, 3) conv_gradient_kernel(const ConvArgs p, const T* x, const T* window_in, const T* dy, const float* dwindow_out,
                                                                     T* dx, float* dwindow_in, float* part)
 {
     pdl_wait();
     pdl_trigger();
+    extern __shared__ __align__(16) uint8_t s_mem[];
     __shared__ float sums[kWarps][(W + 1) * V][33];
     const Place q = place<V>(p);
     float dw[W][V] = {}, db[V] = {};
-    if (q.on && (q.t0 < q.end || q.last)) {
-        float w[W][V], b[V], win[W][V], pend[W][V];
+    if (__any_sync(0xffffffffu, q.on && (q.t0 < q.end || q.last))) {
+        constexpr int G = kGroup;
+        const int n = __reduce_max_sync(0xffffffffu, q.n), t0 = __reduce_max_sync(0xffffffffu, q.on ? q.t0 : 0), t1 = __reduce_max_sync(0xffffffffu, q.on ? q.t1 : 0);
+        const int end = __reduce_max_sync(0xffffffffu, q.on ? q.end : 0), stop = min(t1 + W - 1, end);
+        Feed<T, V, 2> feed;
+        feed.at[0] = x + ((int64_t)t0 * p.N + n) * p.ld_x + q.c;
+        feed.at[1] = dy + ((int64_t)t0 * p.N + n) * p.ld_dy + q.c;
+        feed.step[0] = (int64_t)p.N * p.ld_x;
+        feed.step[1] = (int64_t)p.N * p.ld_dy;
+        feed.begin(reinterpret_cast<Vec<T, V>*>(s_mem) + threadIdx.y * 32 + threadIdx.x, q.on ? stop - t0 : 0);
+        Starts starts;
+        starts.begin(p, n, t0, stop);
+        float w[W][V], b[V], win[W][V], gs[W][V];
         weights(p, q.c, w, b);
         enter<T, V, W>(p, q, x, window_in, win);
-        clear(pend);
-        int since = W;                          // steps since the episode's start; W: further back than any tap
+        clear(gs);
+        uint32_t history = 0;                   // which of the last steps began an episode, the last in bit 0
         // the gradient of input u leaves: it is this run's, or the window's and the run is the first
+        const int64_t step_dx = (int64_t)p.N * p.ld_dx;
+        T* to = dx ? dx + ((int64_t)t0 * p.N + n) * p.ld_dx + q.c : nullptr;      // of the first input that has not left
         auto leave = [&](int u, const float (&g)[V]) {
-            if (u >= q.t0) {
-                if (dx) store_vec<V>(dx + ((size_t)u * p.N + q.n) * p.ld_dx + q.c, g);
-            } else if (q.first && dwindow_in)
-                store_vec<V>(dwindow_in + ((size_t)q.n * (W - 1) + u + W - 1) * p.D + q.c, g);
+            if (u >= t0) {
+                if (dx && q.on) store_vec<V>(to, g);
+                to += step_dx;
+            } else if (q.first && q.on && dwindow_in)
+                store_vec<V>(dwindow_in + ((size_t)n * (W - 1) + u + W - 1) * p.D + q.c, g);
         };
-        constexpr int G = 4;
-        const int stop = min(q.t1 + W - 1, q.end);
-        for (int t = q.t0; t < stop; t += G) {
-            Vec<T, V> rx[G], rg[G];
-            uint8_t st[G];
+        auto slope = [&](auto tap, const float (&raw)[V], float (&g)[V]) {
 #pragma unroll
-            for (int j = 0; j < G; ++j) {
-                const size_t row = (size_t)min(t + j, stop - 1) * p.N + q.n;
-                rx[j] = load_vec<V>(x + row * p.ld_x + q.c);
-                rg[j] = load_vec<V>(dy + row * p.ld_dy + q.c);
-                st[j] = p.starts ? p.starts[row] : 0;
+            for (int i = 0; i < V; ++i) {
+                float a = b[i];
+#pragma unroll
+                for (int k = 0; k < W; ++k) a = fmaf(w[k][i], tap(k, i), a);
+                g[i] = raw[i] * (p.silu ? silu_slope(a) : 1.f);
             }
+        };
+        auto add = [&](auto tap, const float (&g)[V]) {
 #pragma unroll
-            for (int j = 0; j < G; ++j)
-                if (t + j < stop) {
-                    float v[V], g[V];
+            for (int i = 0; i < V; ++i) {
+                db[i] += g[i];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) v[i] = to_float(rx[j].v[i]);
-                    if (st[j]) { clear(win); since = 0; }
-                    else since = min(since + 1, W);
-                    push(win, v);
-                    const bool mine = t + j < q.t1;
-                    const float zero[V] = {};
-                    push(pend, zero);
+                for (int k = 0; k < W; ++k) dw[k][i] = fmaf(g[i], tap(k, i), dw[k][i]);
+            }
+        };
+        for (int t = t0; t < stop; t += G) {
+            float in[2][G][V], v[G + W - 1][V], g[G + W - 1][V];
+            feed.take(in);
+            const uint32_t fresh = starts.take(p, n, stop);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+#pragma unroll
+                for (int k = 0; k < W - 1; ++k) { v[k][i] = win[k + 1][i]; g[k][i] = gs[k + 1][i]; }
+#pragma unroll
+                for (int j = 0; j < G; ++j) v[W - 1 + j][i] = in[0][j][i];
+            }
+            if (!fresh && !(history & ((1u << (W - 1)) - 1)) && t + G <= t1) {
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    auto tap = [&](int k, int i) { return v[j + k][i]; };
+                    slope(tap, in[1][j], g[W - 1 + j]);
+                    add(tap, g[W - 1 + j]);
+                    float r[V];
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        float a = b[i];
+                        r[i] = 0.f;
 #pragma unroll
-                        for (int k = 0; k < W; ++k) a = fmaf(w[k][i], win[k][i], a);
-                        g[i] = to_float(rg[j].v[i]);
-                        if (p.silu) g[i] *= silu_slope(a);
-                        if (mine) {
-                            db[i] += g[i];
-#pragma unroll
-                            for (int k = 0; k < W; ++k) dw[k][i] = fmaf(g[i], win[k][i], dw[k][i]);
-                        }
-#pragma unroll
-                        for (int k = 0; k < W; ++k) pend[k][i] = W - 1 - k <= since ? fmaf(w[k][i], g[i], pend[k][i]) : pend[k][i];
+                        for (int k = 0; k < W; ++k) r[i] = fmaf(w[W - 1 - k][i], g[j + k][i], r[i]);
                     }
-                    leave(t + j - (W - 1), pend[0]);
+                    leave(t + j - (W - 1), r);
                 }
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+#pragma unroll
+                    for (int k = 1; k < W; ++k) { win[k][i] = v[G - 1 + k][i]; gs[k][i] = g[G - 1 + k][i]; }
+                history <<= G;
+            } else
+#pragma unroll
+                for (int j = 0; j < G; ++j)
+                    if (t + j < stop) {
+                        const uint32_t st = fresh >> j & 1;
+                        history = history << 1 | st;
+                        if (st) clear(win);
+                        push(win, v[W - 1 + j]);
+                        auto tap = [&](int k, int i) { return win[k][i]; };
+                        float here[V], r[V];
+                        slope(tap, in[1][j], here);
+                        push(gs, here);
+                        if (t + j < t1) add(tap, here);
+                        bool same = true;       // no start between the input and the step
+#pragma unroll
+                        for (int k = 0; k < W; ++k) {
+                            if (k) same = same && !(history >> (W - 1 - k) & 1);
+#pragma unroll
+                            for (int i = 0; i < V; ++i) r[i] = k == 0 ? w[W - 1][i] * gs[0][i] : same ? fmaf(w[W - 1 - k][i], gs[k][i], r[i]) : r[i];
+                        }
+                        leave(t + j - (W - 1), r);
+                    }
         }
-        if (stop == q.end) {                    // the window after the sequence holds its last inputs
+        if (stop == end) {                      // the last inputs: no more steps, but the window after the sequence holds them
 #pragma unroll
             for (int j = 1; j < W; ++j) {
-                const int u = q.end - W + j;
-                if (u >= q.t1) continue;        // the next run's
-                float g[V];
+                const int u = end - W + j;
+                if (u >= t1 && u >= 0) continue;        // the next run's
+                float r[V];
+                bool same = true;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    g[i] = pend[j][i];
-                    if (dwindow_out && W - 1 - j <= since) g[i] += dwindow_out[((size_t)q.n * (W - 1) + j - 1) * p.D + q.c + i];
+                for (int i = 0; i < V; ++i) r[i] = 0.f;
+#pragma unroll
+                for (int k = 0; k + j < W; ++k) {
+                    if (k) same = same && !(history >> (W - 1 - j - k) & 1);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) r[i] = same ? fmaf(w[W - 1 - k][i], gs[j + k][i], r[i]) : r[i];
                 }
-                leave(u, g);
+                if (dwindow_out && same)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) r[i] += dwindow_out[((size_t)n * (W - 1) + j - 1) * p.D + q.c + i];
+                leave(u, r);
             }
         }
+        if (!q.on)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                db[i] = 0.f;
+#pragma unroll
+                for (int k = 0; k < W; ++k) dw[k][i] = 0.f;
+            }
     }
     if (!part) return;
 #pragma unroll
@@ -305,11 +460,11 @@ __global__ void __launch_bounds__(1024) column_sums_kernel(const ColumnSums p)
     }
 }
 
-// Runs of steps: enough threads for two thousand on every SM, `least` steps at least.
+// Runs of steps: enough threads for 1536 on every SM, which hold 768, `least` steps at least.
 void cut_runs(ConvArgs& p, int V, int least)
 {
     p.lanes = p.D / V;
-    const int64_t want = ceil_div((int64_t)kCoreSms * 2048, (int64_t)p.N * p.lanes);
+    const int64_t want = ceil_div((int64_t)kCoreSms * 1536, (int64_t)p.N * p.lanes);
     const int64_t length = ceil_div(ceil_div(p.T, want), kGroup) * kGroup;
     p.length = (int)(length < least ? least : length);
     p.runs = (int)ceil_div(p.T, p.length);
@@ -352,7 +507,10 @@ hts_status forward(ConvArgs p, int width, const T* x, const T* win, T* y, T* wou
     if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
     return by_width(width, [&](auto k) {
         constexpr int W = decltype(k)::value;
-        HTS_CUDA(launch_pdl(wide ? conv_kernel<T, kVector, W> : conv_kernel<T, 1, W>, dim3((unsigned)blocks), dim3(32, kWarps), 0, s, p, x, win, y, wout));
+        static OncePerDevice allowed[2];
+        auto kernel = wide ? conv_kernel<T, kVector, W> : conv_kernel<T, 1, W>;
+        HTS_CUDA(allow_shared(kernel, allowed[wide]));
+        HTS_CUDA(launch_pdl(kernel, dim3((unsigned)blocks), dim3(32, kWarps), wide ? kFeedBytes<T, kVector, 1> : kFeedBytes<T, 1, 1>, s, p, x, win, y, wout));
         note_launch();
         return HTS_OK;
     });
@@ -383,8 +541,11 @@ hts_status gradient(ConvArgs p, int width, const T* x, const T* win, const T* dy
     const bool sums = dw || db;
     const hts_status st = by_width(width, [&](auto k) {
         constexpr int W = decltype(k)::value;
-        HTS_CUDA(launch_pdl(wide ? conv_gradient_kernel<T, kGradVector, W> : conv_gradient_kernel<T, 1, W>, dim3((unsigned)blocks), dim3(32, kWarps), 0, s, p, x, win, dy,
-                            dwout, dx, dwin, sums ? part : nullptr));
+        static OncePerDevice allowed[2];
+        auto kernel = wide ? conv_gradient_kernel<T, kGradVector, W> : conv_gradient_kernel<T, 1, W>;
+        HTS_CUDA(allow_shared(kernel, allowed[wide]));
+        HTS_CUDA(launch_pdl(kernel, dim3((unsigned)blocks), dim3(32, kWarps), wide ? kFeedBytes<T, kGradVector, 2> : kFeedBytes<T, 1, 2>, s, p, x, win, dy, dwout, dx, dwin,
+                            sums ? part : nullptr));
         note_launch();
         return HTS_OK;
     });

@@ -47,6 +47,16 @@ __device__ __forceinline__ void copy16(void* smem, const void* from, bool on)   
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(from), "r"(on ? 16 : 0) : "memory");
 }
+// A vector on its way to shared memory, for the thread that asks for it; what has fewer than four bytes goes through a register.
+template <int V, typename T>
+__device__ __forceinline__ void copy_vec(Vec<T, V>* smem, const T* from)
+{
+    constexpr int BYTES = sizeof(Vec<T, V>);
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(smem);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(BYTES) : "memory");
+    else *smem = load_vec<V>(from);
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
