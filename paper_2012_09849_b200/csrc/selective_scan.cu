@@ -51,6 +51,12 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
+struct Quad { f32x2 x, y; };
+__device__ __forceinline__ Quad load_quad(const float* at)
+{
+    const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(at);
+    return {v.x, v.y};
+}
 // exp(delta A) of a pair of states, a2 = A log2(e).  ex2.approx comes out 2e-8 too small on average for exponents between -1 and 0
 // (a third of a last place; measured over each part of that range), and a decay near 1 acts for hundreds of steps, so that the
 // sums drift: states of a 128-step rollout off by 2.1e-6.  Adding 2.3e-8 to the exponent, in the multiply-add that forms it, takes
@@ -124,12 +130,14 @@ template <typename T, bool WIDE, int ROWS, int CB>
 __device__ __forceinline__ void copy_rows(const ScanArgs& p, T (*to)[CB], const T* from, int64_t ld, int n, int t, int end, int c0)
 {
     constexpr int PER = WIDE ? 16 / sizeof(T) : 1, PIECES = CB / PER;
+    const T* base = from + ((int64_t)t * p.N + n) * ld;             // the same for the warp; what differs fits 32 bits (kMostInStep)
+    const int step = p.N * (int)ld;
 #pragma unroll
     for (int e0 = 0; e0 < ROWS * PIECES; e0 += kThreads) {
         const int e = e0 + threadIdx.x, j = e / PIECES, c = e % PIECES * PER;
         if (ROWS * PIECES % kThreads && e >= ROWS * PIECES) break;
         const bool on = t + j < end && c0 + c < p.D;
-        const T* at = from + (on ? ((int64_t)(t + j) * p.N + n) * ld + c0 + c : 0);
+        const T* at = base + (on ? j * step + c0 + c : 0);
         if (WIDE) copy16(&to[j][c], at, on);
         else to[j][c] = on ? *at : from_float<T>(0.f);
     }
@@ -177,9 +185,9 @@ __global__ void __launch_bounds__(kThreads, 5) scan_kernel(const ScanArgs p, con
         for (int i = 0; i < BC; ++i) {
             const int e = threadIdx.x + i * kThreads, s = e % SP;
             if (s < p.S && t + e / SP < t1) {
-                const int64_t row = (int64_t)(t + e / SP) * p.N + n;
-                rb[i] = b[row * p.ld_b + s];
-                if (MODE != MAPS) rc[i] = c[row * p.ld_c + s];
+                const int64_t row = (int64_t)t * p.N + n;
+                rb[i] = (b + row * p.ld_b)[e / SP * p.N * (int)p.ld_b + s];
+                if (MODE != MAPS) rc[i] = (c + row * p.ld_c)[e / SP * p.N * (int)p.ld_c + s];
             }
         }
         rst = start_at(p, n, t, t1);
@@ -229,11 +237,11 @@ __global__ void __launch_bounds__(kThreads, 5) scan_kernel(const ScanArgs p, con
                 f32x2 acc[2] = {both(0.f), both(0.f)};
 #pragma unroll
                 for (int i = 0; i < SPT / 2; i += 2) {
-                    const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[buf][j][s0 + 2 * i]);
+                    const Quad bv = load_quad(&sb[buf][j][s0 + 2 * i]);
                     const f32x2 bb[2] = {bv.x, bv.y};
-                    f32x2 cc[2] = {0, 0};
+                    f32x2 cc[2] = {both(0.f), both(0.f)};
                     if (MODE != MAPS) {
-                        const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[buf][j][s0 + 2 * i]);
+                        const Quad cv = load_quad(&sc[buf][j][s0 + 2 * i]);
                         cc[0] = cv.x; cc[1] = cv.y;
                     }
 #pragma unroll
@@ -383,7 +391,7 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const ScanArgs p, const 
 // ---- gradient ------------------------------------------------------------------------------------------------------------
 struct GradArgs {
     int64_t ld_dy, ld_dx, ld_ddt, ld_dz;
-    float *checks;                              // states at the chunks' first steps, [block][chunk][quarter][thread] of float4
+    float *checks;                              // states at the chunks' first steps, [block][chunk][2][thread] of float4
     float *part_bc;                             // [channel block][row][2 SP]
     float *part_ch;                             // [run][N][D S + 2 D]: dA, dD, d(dt_bias)
     const float *first, *incoming;              // [run][N][D][S]: states at the runs' first steps; gradients from behind the runs
@@ -391,286 +399,305 @@ struct GradArgs {
     int chunks;                                 // of kChunk steps, per run
 };
 constexpr int kChunk = 8;
+template <int LS> struct GradientShape {
+    static constexpr int SP = 4 * LS, CB = 2 * kThreads / LS;                   // states with the padding, channels of a block
+};
+template <typename T, int LS> struct GradientShared {
+    static constexpr int SP = GradientShape<LS>::SP, CB = GradientShape<LS>::CB;
+    float4 du[kChunk][CB / 2];                  // of two channels: delta, delta; delta x, delta x
+    float g[kChunk][CB], gb[kChunk][CB], gk[kChunk][CB], y[kChunk][CB];
+    float b[kChunk][SP], c[kChunk][SP], red[kThreads / 32][kChunk][2 * SP];
+    T tile[2][4][kChunk][CB];                   // x, dt, z, dy
+};
 
 // A run's steps in chunks of kChunk.  Forward through the run, the state at every chunk's first step goes to memory; then the
-// chunks are taken from the last to the first: their states are computed again and kept in shared memory, and the gradient
-// of the state walks back over them.  Sums over channels (dB, dC) are taken from shared memory too: a thread takes four
-// states of a step and adds the products of a share of the block's channels, which costs one load and two packed
-// multiply-adds for four terms, where exchanges between lanes would take two of each for every term.
-template <typename T, int SPT, int LS, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 4) scan_gradient_kernel(const ScanArgs p, const GradArgs q, const T* x, const T* dt, const T* b, const T* c, const T* z,
-                                                                 const T* dy, T* dx, T* ddt, T* dz)
+// chunks are taken from the last to the first: their states are computed again, into registers, and the gradient of the state walks
+// back over them.
+//
+// A thread has four states of two neighbouring channels, LS lanes a pair of channels.  What has to be added over states (three sums a
+// channel) crosses LS lanes, what has to be added over channels (dB and dC, eight sums, two channels of which meet in the thread)
+// the others: in the first exchanges of each each lane keeps half of the sums and hands on the other half.  With eight states of one
+// channel in a thread, states and gradients in shared memory and the sums over channels read from there, shared memory
+// bounded it (105 accesses a warp and step): 1165 us for 128 x 256 steps of 1024 channels and 16 states, now @G.
+template <typename T, int LS, bool WIDE>
+__global__ void __launch_bounds__(kThreads, VGB) scan_gradient_kernel(const ScanArgs p, const GradArgs q, const T* x, const T* dt, const T* b, const T* c, const T* z,
+                                                                    const T* dy, T* dx, T* ddt, T* dz)
 {
-    constexpr int SP = SPT * LS, CB = kThreads / LS, Q = SPT / 4, ITEMS = kChunk * CB / kThreads;
+    using S = GradientShape<LS>;
+    constexpr int SP = S::SP, CB = S::CB, ITEMS = kChunk * CB / kThreads, APART = kThreads / CB, BC = (kChunk * SP + kThreads - 1) / kThreads;
     extern __shared__ __align__(16) float s_mem[];
-    float4* hs = reinterpret_cast<float4*>(s_mem);                              // [kChunk][Q][kThreads]: states, then their gradients
-    float* s_delta = s_mem + kChunk * SPT * kThreads;                           // [kChunk][CB] each
-    float *s_x = s_delta + kChunk * CB, *s_g = s_x + kChunk * CB, *s_gb = s_g + kChunk * CB, *s_gk = s_gb + kChunk * CB, *s_y = s_gk + kChunk * CB;
-    float(*sb)[SP] = reinterpret_cast<float(*)[SP]>(s_y + kChunk * CB);
-    float(*sc)[SP] = sb + kChunk;
-    T(*tile)[4][kChunk][CB] = reinterpret_cast<T(*)[4][kChunk][CB]>(sc + kChunk);      // [2]: x, dt, z, dy
+    GradientShared<T, LS>& sh = *reinterpret_cast<GradientShared<T, LS>*>(s_mem);
     static_assert(kChunk <= 8, "start_at");
     pdl_wait();
     pdl_trigger();
-    const int tid = threadIdx.x, across = (p.D + CB - 1) / CB, cb = (int)(blockIdx.x % across);
+    const int tid = threadIdx.x, lane = tid & 31, across = (p.D + CB - 1) / CB, cb = (int)(blockIdx.x % across);
     const int n = (int)(blockIdx.x / across % p.N), run = (int)(blockIdx.x / across / p.N);
-    const int sub = tid % LS, cl = tid / LS, s0 = sub * SPT, own = cb * CB + cl;
-    const bool on = own < p.D;
-    const int ch = on ? own : 0, channels = min(CB, p.D - cb * CB);
+    const int sub = tid % LS, pc = tid / LS, s0 = sub * 4, c0 = cb * CB + 2 * pc;
     const int end = uniform(steps_of(p.lengths, n, p.T));
     const int t0 = min(run * p.length, end), t1 = min(t0 + p.length, end), chunks = (t1 - t0 + kChunk - 1) / kChunk;
     // the channel whose inputs and outputs this thread converts: the same for all its items
-    const int ic = tid % CB, ich = min(cb * CB + ic, p.D - 1);
+    const int ic = tid % CB, first_row = tid / CB, ich = min(cb * CB + ic, p.D - 1);
     const bool ion = cb * CB + ic < p.D;
     const float iskip = p.d ? p.d[ich] : 0.f, ibias = p.dt_bias ? p.dt_bias[ich] : 0.f;
     const size_t row0 = (size_t)run * p.N + n;
 
-    f32x2 a2[SPT / 2], h[SPT / 2], carry[SPT / 2], da[SPT / 2];
-    load_decays<SPT>(p, ch, s0, on, a2);
-    load_states<SPT>(p, q.first, row0, ch, s0, on, h);
-    load_states<SPT>(p, q.incoming, row0, ch, s0, on, carry);
+    f32x2 a2[2][2], h0[2][2], carry[2][2], da[2][2];
 #pragma unroll
-    for (int i = 0; i < SPT / 2; ++i) da[i] = both(0.f);
+    for (int e = 0; e < 2; ++e) {
+        const bool on = c0 + e < p.D;
+        load_decays<4>(p, on ? c0 + e : 0, s0, on, a2[e]);
+        load_states<4>(p, q.first, row0, on ? c0 + e : 0, s0, on, h0[e]);
+        load_states<4>(p, q.incoming, row0, on ? c0 + e : 0, s0, on, carry[e]);
+        da[e][0] = da[e][1] = both(0.f);
+    }
     float dskip = 0.f, dbias = 0.f;
-    float4* checks = reinterpret_cast<float4*>(q.checks) + (size_t)blockIdx.x * q.chunks * Q * kThreads + tid;
+    float4* checks = reinterpret_cast<float4*>(q.checks) + (size_t)blockIdx.x * q.chunks * 2 * kThreads + tid;
 
     uint32_t fresh = 0;                                                         // the chunk's steps that begin an episode
-    auto advance = [&](auto with_starts, int j, f32x2 (&h)[SPT / 2]) {          // one step of the state
-        const int at = j * CB + cl;
-        const float delta = s_delta[at];
-        const f32x2 d2 = both(delta), u2 = both(delta * s_x[at]);
-        if (decltype(with_starts)::value && (fresh >> j & 1))
-#pragma unroll
-            for (int i = 0; i < SPT / 2; ++i) h[i] = both(0.f);
-#pragma unroll
-        for (int i = 0; i < SPT / 2; i += 2) {
-            const ulonglong2 bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 2 * i]);
-            h[i] = fma2(decay_pair(d2, a2[i]), h[i], mul2(u2, bv.x));
-            h[i + 1] = fma2(decay_pair(d2, a2[i + 1]), h[i + 1], mul2(u2, bv.y));
-        }
-    };
     auto by_starts = [&](auto f) {                                              // a chunk without one has no branch between its steps
         if (fresh) f(std::true_type());
         else f(std::false_type());
     };
+    auto advance = [&](auto with_starts, int j, const f32x2 (&from)[2][2], f32x2 (&to)[2][2]) {
+        const float4 du = sh.du[j][pc];
+        const Quad bv = load_quad(&sh.b[j][s0]);
+        const bool st = decltype(with_starts)::value && (fresh >> j & 1);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const f32x2 d2 = both(e ? du.y : du.x), u2 = both(e ? du.w : du.z);
+            to[e][0] = fma2(decay_pair(d2, a2[e][0]), st ? both(0.f) : from[e][0], mul2(u2, bv.x));
+            to[e][1] = fma2(decay_pair(d2, a2[e][1]), st ? both(0.f) : from[e][1], mul2(u2, bv.y));
+        }
+    };
     // A chunk's inputs are on their way to shared memory, B, C and the starts to registers, while the chunk before is worked on.
-    constexpr int BC = (kChunk * SP + kThreads - 1) / kThreads;
     T rb[BC], rc[BC];
     uint8_t rst = 0;
-    const int first_row = tid / CB;
-    constexpr int APART = kThreads / CB;
-    const int64_t my_row = (int64_t)first_row * p.N;
     auto ask = [&](int t, int slot, bool all) {
-        copy_rows<T, WIDE, kChunk, CB>(p, tile[slot][0], x, p.ld_x, n, t, t1, cb * CB);
-        copy_rows<T, WIDE, kChunk, CB>(p, tile[slot][1], dt, p.ld_dt, n, t, t1, cb * CB);
-        if (all && z) copy_rows<T, WIDE, kChunk, CB>(p, tile[slot][2], z, p.ld_z, n, t, t1, cb * CB);
-        if (all) copy_rows<T, WIDE, kChunk, CB>(p, tile[slot][3], dy, q.ld_dy, n, t, t1, cb * CB);
+        copy_rows<T, WIDE, kChunk, CB>(p, sh.tile[slot][0], x, p.ld_x, n, t, t1, cb * CB);
+        copy_rows<T, WIDE, kChunk, CB>(p, sh.tile[slot][1], dt, p.ld_dt, n, t, t1, cb * CB);
+        if (all && z) copy_rows<T, WIDE, kChunk, CB>(p, sh.tile[slot][2], z, p.ld_z, n, t, t1, cb * CB);
+        if (all) copy_rows<T, WIDE, kChunk, CB>(p, sh.tile[slot][3], dy, q.ld_dy, n, t, t1, cb * CB);
         copies_commit();
 #pragma unroll
         for (int i = 0; i < BC; ++i) {
             const int e = tid + i * kThreads, s = e % SP;
             if (s < p.S && t + e / SP < t1) {
-                const int64_t row = (int64_t)(t + e / SP) * p.N + n;
-                rb[i] = b[row * p.ld_b + s];
-                if (all) rc[i] = c[row * p.ld_c + s];
+                const int64_t row = (int64_t)t * p.N + n;
+                rb[i] = (b + row * p.ld_b)[e / SP * p.N * (int)p.ld_b + s];
+                if (all) rc[i] = (c + row * p.ld_c)[e / SP * p.N * (int)p.ld_c + s];
             }
         }
         rst = start_at(p, n, t, t1);
     };
-    auto stage_bc_starts = [&](int t, bool all) {                               // zero behind the last state and step
+    auto arrive = [&](int t, bool all) {                                        // B and C: zero behind the last state and step
+        copies_wait<0>();
 #pragma unroll
         for (int i = 0; i < BC; ++i) {
             const int e = tid + i * kThreads, j = e / SP, s = e % SP;
             if (kChunk * SP % kThreads && e >= kChunk * SP) break;
             const bool live = s < p.S && t + j < t1;
-            sb[j][s] = live ? to_float(rb[i]) : 0.f;
-            if (all) sc[j][s] = live ? to_float(rc[i]) : 0.f;
+            sh.b[j][s] = live ? to_float(rb[i]) : 0.f;
+            if (all) sh.c[j][s] = live ? to_float(rc[i]) : 0.f;
         }
         fresh = __ballot_sync(0xffffffffu, rst != 0);
+        __syncthreads();                                                        // everybody's copies
     };
 
     if (chunks) ask(t0, 0, chunks == 1);
     for (int k = 0; k < chunks; ++k) {                                          // states at the chunks' first steps
 #pragma unroll
-        for (int i = 0; i < Q; ++i)
-            checks[(size_t)(k * Q + i) * kThreads] = make_float4(lane_of(h[2 * i], 0), lane_of(h[2 * i], 1), lane_of(h[2 * i + 1], 0), lane_of(h[2 * i + 1], 1));
+        for (int e = 0; e < 2; ++e)
+            checks[(size_t)(2 * k + e) * kThreads] = make_float4(lane_of(h0[e][0], 0), lane_of(h0[e][0], 1), lane_of(h0[e][1], 0), lane_of(h0[e][1], 1));
         if (k == chunks - 1) break;                                             // that one's steps come next
         const int t = t0 + k * kChunk;
-        copies_wait<0>();
-        stage_bc_starts(t, false);
-        __syncthreads();                                                        // everybody's copies
+        arrive(t, false);
         ask(t + kChunk, (k + 1) & 1, k + 2 == chunks);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int e = tid + i * kThreads;
-            const float raw = to_float(tile[k & 1][1][e / CB][ic]) + ibias;
-            s_delta[e] = ion ? (p.softplus ? softplus(raw) : raw) : 0.f;
-            s_x[e] = ion ? to_float(tile[k & 1][0][e / CB][ic]) : 0.f;
+            const int j = first_row + i * APART;
+            const float raw = to_float(sh.tile[k & 1][1][j][ic]) + ibias, delta = ion ? (p.softplus ? softplus(raw) : raw) : 0.f;
+            float* du = &sh.du[j][ic >> 1].x + (ic & 1);
+            du[0] = delta;
+            du[2] = delta * to_float(sh.tile[k & 1][0][j][ic]);
         }
         __syncthreads();
         by_starts([&](auto with_starts) {
 #pragma unroll
-            for (int j = 0; j < kChunk; ++j) advance(with_starts, j, h);
+            for (int j = 0; j < kChunk; ++j) advance(with_starts, j, h0, h0);
         });
         __syncthreads();
     }
-    f32x2 ahead[SPT / 2];                                                       // the next chunk's first state
-#pragma unroll
-    for (int i = 0; i < SPT / 2; ++i) ahead[i] = h[i];
+
     for (int k = chunks - 1; k >= 0; --k) {
         const int t = t0 + k * kChunk;
-        copies_wait<0>();
-        stage_bc_starts(t, true);
-        __syncthreads();                                                        // everybody's copies
+        arrive(t, true);
         float slope_dt[ITEMS], slope_z[ITEMS];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {                                       // steps behind the end: nothing in, all kept
-            const int e = tid + i * kThreads;
-            const bool live = ion && t + e / CB < t1;
-            float delta = 0.f, xv = 0.f, g = 0.f;
+            const int j = first_row + i * APART;
+            const bool live = ion && t + j < t1;
+            float delta = 0.f, u = 0.f, g = 0.f;
             slope_dt[i] = 1.f; slope_z[i] = 0.f;
             if (live) {
-                const float raw = to_float(tile[k & 1][1][e / CB][ic]) + ibias;
+                const float raw = to_float(sh.tile[k & 1][1][j][ic]) + ibias, xv = to_float(sh.tile[k & 1][0][j][ic]);
                 delta = p.softplus ? softplus(raw, &slope_dt[i]) : raw;
-                xv = to_float(tile[k & 1][0][e / CB][ic]);
-                g = to_float(tile[k & 1][3][e / CB][ic]);
+                u = delta * xv;
+                g = to_float(sh.tile[k & 1][3][j][ic]);
                 if (z) {
-                    const float zv = to_float(tile[k & 1][2][e / CB][ic]), sg = sigmoid(zv);
+                    const float zv = to_float(sh.tile[k & 1][2][j][ic]), sg = sigmoid(zv);
                     slope_z[i] = g * (sg * (1.f + zv * (1.f - sg)));
                     g *= zv * sg;
                 }
                 dskip = fmaf(g, xv, dskip);
             }
-            s_delta[e] = delta; s_x[e] = xv; s_g[e] = g;
+            float* du = &sh.du[j][ic >> 1].x + (ic & 1);
+            du[0] = delta;
+            du[2] = u;
+            sh.g[j][ic] = g;
         }
-        f32x2 h0[SPT / 2];
-#pragma unroll
-        for (int i = 0; i < SPT / 2; ++i) h[i] = h0[i] = ahead[i];
         __syncthreads();
+        f32x2 ahead[2][2];                                                      // the first state of the chunk that comes next
         if (k) {
             ask(t - kChunk, (k - 1) & 1, true);
 #pragma unroll
-            for (int i = 0; i < Q; ++i) {
-                const float4 v = checks[(size_t)((k - 1) * Q + i) * kThreads];
-                ahead[2 * i] = pair(v.x, v.y);
-                ahead[2 * i + 1] = pair(v.z, v.w);
+            for (int e = 0; e < 2; ++e) {
+                const float4 v = checks[(size_t)(2 * (k - 1) + e) * kThreads];
+                ahead[e][0] = pair(v.x, v.y);
+                ahead[e][1] = pair(v.z, v.w);
             }
         }
+        // half a chunk at a time, so that its states fit the registers beside the rest
         by_starts([&](auto with_starts) {
+#pragma unroll 1
+            for (int from = kChunk / 2; from >= 0; from -= kChunk / 2) {
+            f32x2 before[2][2], h[kChunk / 2][2][2];
 #pragma unroll
-            for (int j = 0; j < kChunk; ++j) {                                  // the chunk's states, and the sums over them
-                advance(with_starts, j, h);
-                f32x2 acc = both(0.f);
+            for (int e = 0; e < 2; ++e) { before[e][0] = h0[e][0]; before[e][1] = h0[e][1]; }
+            if (from)
 #pragma unroll
-                for (int i = 0; i < Q; ++i) {
-                    const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]);
-                    acc = fma2(cv.x, h[2 * i], acc);
-                    acc = fma2(cv.y, h[2 * i + 1], acc);
-                    *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(h[2 * i], h[2 * i + 1]);
-                }
-                float v = lane_of(acc, 0) + lane_of(acc, 1);
+                for (int j = 0; j < kChunk / 2; ++j) advance(with_starts, j, before, before);
 #pragma unroll
-                for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (sub == 0) s_y[j * CB + cl] = v;
-            }
-        });
-        __syncthreads();
-        // sums over the block's channels of weight x what hs holds, four states of a step to a thread and a share of the channels
-        auto over_channels = [&](auto weight, int half) {
-            constexpr int QUADS = kChunk * SP / 4, WAYS = QUADS >= kThreads ? 1 : kThreads / QUADS < 8 ? kThreads / QUADS : 8;
-            static_assert(QUADS * WAYS % 32 == 0 && QUADS * WAYS <= kThreads, "whole warps, one turn");
-            if (tid < QUADS * WAYS) {           // eight neighbouring lanes read eight neighbouring pieces of 16 bytes
-                const int way = tid % WAYS, lane = tid / WAYS % LS, i = tid / (WAYS * LS) % Q, j = tid / (WAYS * LS * Q), quad = lane * Q + i;
-                const int slot = (j * Q + i) * kThreads + lane;
-                f32x2 u = both(0.f), v = both(0.f);
-#pragma unroll 4
-                for (int l = way; l < channels; l += WAYS) {
-                    const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&hs[slot + l * LS]);
-                    const f32x2 f = both(weight(j * CB + l));
-                    u = fma2(f, w.x, u);
-                    v = fma2(f, w.y, v);
-                }
-                float r[4] = {lane_of(u, 0), lane_of(u, 1), lane_of(v, 0), lane_of(v, 1)};
+            for (int i = 0; i < kChunk / 2; ++i) advance(with_starts, from + i, i ? h[i - 1] : before, h[i]);
 #pragma unroll
-                for (int o = 1; o < WAYS; o <<= 1)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) r[k] += __shfl_xor_sync(0xffffffffu, r[k], o);
-                if (way == 0 && t + j < t1)
-                    *reinterpret_cast<float4*>(q.part_bc + (((size_t)cb * p.T + t + j) * p.N + n) * (2 * SP) + half * SP + 4 * quad) = make_float4(r[0], r[1], r[2], r[3]);
-            }
-        };
-        over_channels([&](int at) { return s_g[at]; }, 1);
-        __syncthreads();
-        by_starts([&](auto with_starts) {
-#pragma unroll
-            for (int j = kChunk - 1; j >= 0; --j) {                             // back over the chunk
-                const int at = j * CB + cl;
-                const float delta = s_delta[at];
-                const f32x2 d2 = both(delta), g2 = both(s_g[at]);
+            for (int at = kChunk / 2 - 1; at >= 0; --at) {                      // back over its steps
+                const int j = from + at;
+                const float4 du = sh.du[j][pc];
+                const float2 gv = *reinterpret_cast<const float2*>(&sh.g[j][2 * pc]);
+                const Quad bv = load_quad(&sh.b[j][s0]), cv = load_quad(&sh.c[j][s0]);
                 const bool st = decltype(with_starts)::value && (fresh >> j & 1);
-                f32x2 gb = both(0.f), gk = both(0.f);
+                const f32x2 b2[2] = {bv.x, bv.y}, c2[2] = {cv.x, cv.y};
+                f32x2 db[2], dc[2];
+                float sums[2][3];                                               // of a channel: G B, G kept A, C h
 #pragma unroll
-                for (int i = 0; i < Q; ++i) {
-                    const ulonglong2 cv = *reinterpret_cast<const ulonglong2*>(&sc[j][s0 + 4 * i]), bv = *reinterpret_cast<const ulonglong2*>(&sb[j][s0 + 4 * i]);
-                    ulonglong2 old = j ? *reinterpret_cast<const ulonglong2*>(&hs[((j - 1) * Q + i) * kThreads + tid]) : make_ulonglong2(h0[2 * i], h0[2 * i + 1]);
-                    if (st) old = make_ulonglong2(0, 0);
-                    const f32x2 c2[2] = {cv.x, cv.y}, b2[2] = {bv.x, bv.y}, o2[2] = {old.x, old.y};
-                    f32x2 grad[2];
+                for (int e = 0; e < 2; ++e) {
+                    const f32x2 d2 = both(e ? du.y : du.x), u2 = both(e ? du.w : du.z), g2 = both(e ? gv.y : gv.x);
+                    f32x2 gb, gk, y;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int w = 2 * i + e;
-                        const f32x2 decay = decay_pair(d2, a2[w]);
-                        grad[e] = fma2(g2, c2[e], carry[w]);
-                        const f32x2 flow = mul2(decay, grad[e]), kept = mul2(flow, o2[e]);
-                        gk = fma2(a2[w], kept, gk);
-                        da[w] = fma2(d2, kept, da[w]);
-                        gb = fma2(grad[e], b2[e], gb);
-                        carry[w] = st ? both(0.f) : flow;
+                    for (int i = 0; i < 2; ++i) {
+                        const f32x2 old = st ? both(0.f) : at ? h[at - 1][e][i] : before[e][i];
+                        const f32x2 grad = fma2(g2, c2[i], carry[e][i]), flow = mul2(decay_pair(d2, a2[e][i]), grad), kept = mul2(flow, old);
+                        gk = i ? fma2(a2[e][i], kept, gk) : mul2(a2[e][i], kept);
+                        gb = i ? fma2(grad, b2[i], gb) : mul2(grad, b2[i]);
+                        y = i ? fma2(c2[i], h[at][e][i], y) : mul2(c2[i], h[at][e][i]);
+                        da[e][i] = fma2(d2, kept, da[e][i]);
+                        db[i] = e ? fma2(grad, u2, db[i]) : mul2(grad, u2);
+                        dc[i] = e ? fma2(h[at][e][i], g2, dc[i]) : mul2(h[at][e][i], g2);
+                        carry[e][i] = st ? both(0.f) : flow;
                     }
-                    *reinterpret_cast<ulonglong2*>(&hs[(j * Q + i) * kThreads + tid]) = make_ulonglong2(grad[0], grad[1]);
+                    sums[e][0] = lane_of(gb, 0) + lane_of(gb, 1);
+                    sums[e][1] = lane_of(gk, 0) + lane_of(gk, 1);
+                    sums[e][2] = lane_of(y, 0) + lane_of(y, 1);
                 }
-                float vb = lane_of(gb, 0) + lane_of(gb, 1), vk = lane_of(gk, 0) + lane_of(gk, 1);
+                // over the states: lanes of odd `sub` go on with the second channel
+                const bool odd = sub & 1;
+                float mine[3];
 #pragma unroll
-                for (int o = 1; o < LS; o <<= 1) { vb += __shfl_xor_sync(0xffffffffu, vb, o); vk += __shfl_xor_sync(0xffffffffu, vk, o); }
-                if (sub == 0) { s_gb[at] = vb; s_gk[at] = vk; }
+                for (int i = 0; i < 3; ++i) mine[i] = (odd ? sums[1][i] : sums[0][i]) + __shfl_xor_sync(0xffffffffu, odd ? sums[0][i] : sums[1][i], 1);
+#pragma unroll
+                for (int o = 2; o < LS; o <<= 1)
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) mine[i] += __shfl_xor_sync(0xffffffffu, mine[i], o);
+                if (sub < 2) {
+                    sh.gb[j][2 * pc + sub] = mine[0];
+                    sh.gk[j][2 * pc + sub] = mine[1];
+                    sh.y[j][2 * pc + sub] = mine[2];
+                }
+                // over the channels: the upper half of the warp goes on with dC, every second quarter with the last two states, ...
+                float r[4];
+                const bool up = lane & 16;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float vb = lane_of(db[i / 2], i & 1), vc = lane_of(dc[i / 2], i & 1);
+                    r[i] = (up ? vc : vb) + __shfl_xor_sync(0xffffffffu, up ? vb : vc, 16);
+                }
+                float* red = &sh.red[tid >> 5][j][(up ? SP : 0) + s0];
+                if constexpr (LS == 16) *reinterpret_cast<float4*>(red) = make_float4(r[0], r[1], r[2], r[3]);
+                else {
+                    const bool second = lane & 8;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) r[i] = (second ? r[2 + i] : r[i]) + __shfl_xor_sync(0xffffffffu, second ? r[i] : r[2 + i], 8);
+                    red += second ? 2 : 0;
+                    if constexpr (LS == 8) *reinterpret_cast<float2*>(red) = make_float2(r[0], r[1]);
+                    else {
+                        const bool last = lane & 4;
+                        r[0] = (last ? r[1] : r[0]) + __shfl_xor_sync(0xffffffffu, last ? r[0] : r[1], 4);
+                        if constexpr (LS == 2) r[0] += __shfl_xor_sync(0xffffffffu, r[0], 2);
+                        if (LS == 4 || !(lane & 2)) red[last ? 1 : 0] = r[0];
+                    }
+                }
+            }
             }
         });
         __syncthreads();
-        over_channels([&](int at) { return s_delta[at] * s_x[at]; }, 0);
+        for (int e = tid; e < kChunk * 2 * SP; e += kThreads) {                 // the warps' sums over their channels
+            const int j = e / (2 * SP), s = e % (2 * SP);
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < kThreads / 32; ++w) v += sh.red[w][j][s];
+            if (t + j < t1) (q.part_bc + (((int64_t)cb * p.T + t) * p.N + n) * (2 * SP))[j * p.N * 2 * SP + s] = v;
+        }
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int e = tid + i * kThreads;
-            if (ion && t + e / CB < t1) {
-                const int64_t row = (int64_t)(t + i * APART) * p.N + n;
-                const float xv = s_x[e], gb = s_gb[e];
-                const float dd = fmaf(xv, gb, s_gk[e] * (1.f / kLog2e)) * slope_dt[i];       // a2 is A log2(e)
+            const int j = first_row + i * APART;
+            if (ion && t + j < t1) {
+                const int64_t row = (int64_t)t * p.N + n;
+                const float xv = to_float(sh.tile[k & 1][0][j][ic]), gb = sh.gb[j][ic], delta = (&sh.du[j][ic >> 1].x)[ic & 1];
+                const float dd = fmaf(xv, gb, sh.gk[j][ic] * (1.f / kLog2e)) * slope_dt[i];      // a2 is A log2(e)
                 dbias += dd;
-                if (dx) (dx + my_row * q.ld_dx + ich)[row * q.ld_dx] = from_float<T>(fmaf(s_delta[e], gb, iskip * s_g[e]));
-                if (ddt) (ddt + my_row * q.ld_ddt + ich)[row * q.ld_ddt] = from_float<T>(dd);
-                if (dz) (dz + my_row * q.ld_dz + ich)[row * q.ld_dz] = from_float<T>(slope_z[i] * fmaf(iskip, xv, s_y[e]));
+                if (dx) (dx + row * q.ld_dx)[j * p.N * (int)q.ld_dx + ich] = from_float<T>(fmaf(delta, gb, iskip * sh.g[j][ic]));
+                if (ddt) (ddt + row * q.ld_ddt)[j * p.N * (int)q.ld_ddt + ich] = from_float<T>(dd);
+                if (dz) (dz + row * q.ld_dz)[j * p.N * (int)q.ld_dz + ich] = from_float<T>(slope_z[i] * fmaf(iskip, xv, sh.y[j][ic]));
             }
         }
         __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { h0[e][0] = ahead[e][0]; h0[e][1] = ahead[e][1]; }
     }
 
-    if (run == 0 && q.dstate_in) store_states<SPT>(p, q.dstate_in, n, ch, s0, on, carry);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const bool on = c0 + e < p.D;
+        if (run == 0 && q.dstate_in) store_states<4>(p, q.dstate_in, n, on ? c0 + e : 0, s0, on, carry[e]);
+        if (q.part_ch) store_states<4>(p, q.part_ch + row0 * ((size_t)p.D * p.S + 2 * p.D), 0, on ? c0 + e : 0, s0, on, da[e]);
+    }
     if (q.part_ch) {
-        float* part = q.part_ch + row0 * ((size_t)p.D * p.S + 2 * p.D);
-        store_states<SPT>(p, part, 0, ch, s0, on, da);
-        s_gb[tid] = dskip;                                                      // chunks hold kThreads items at least
-        s_gk[tid] = dbias;
+        float *part = q.part_ch + row0 * ((size_t)p.D * p.S + 2 * p.D), *sums = &sh.gb[0][0];       // kChunk CB of them, kThreads at least
+        sums[tid] = dskip;
         __syncthreads();
         if (tid < CB && ion) {
 #pragma unroll
-            for (int i = 1; i < LS; ++i) { dskip += s_gb[tid + i * CB]; dbias += s_gk[tid + i * CB]; }
+            for (int i = 1; i < APART; ++i) dskip += sums[tid + i * CB];
             part[(size_t)p.D * p.S + ich] = dskip;
+        }
+        __syncthreads();
+        sums[tid] = dbias;
+        __syncthreads();
+        if (tid < CB && ion) {
+#pragma unroll
+            for (int i = 1; i < APART; ++i) dbias += sums[tid + i * CB];
             part[(size_t)p.D * p.S + p.D + ich] = dbias;
         }
     }
-}
-template <typename T, int SPT, int LS> constexpr size_t gradient_shared()
-{
-    return (size_t)(kChunk * SPT * kThreads + 6 * kChunk * (kThreads / LS) + 2 * kChunk * SPT * LS) * 4 + 8 * kChunk * (kThreads / LS) * sizeof(T);
 }
 
 // dB and dC: the channel blocks' parts added in order.
@@ -699,11 +726,7 @@ Shape scan_shape(int S)
     if (S <= 8) return {8, 1};
     return {16, S <= 16 ? 1 : S <= 32 ? 2 : 4};
 }
-Shape gradient_shape(int S)
-{
-    if (S <= 4) return {4, 1};
-    return {8, S <= 8 ? 1 : S <= 16 ? 2 : S <= 32 ? 4 : 8};
-}
+int gradient_lanes(int S) { return S <= 8 ? 2 : S <= 16 ? 4 : S <= 32 ? 8 : 16; }
 template <typename F>
 hts_status by_scan_shape(int S, F f)
 {
@@ -715,14 +738,14 @@ hts_status by_scan_shape(int S, F f)
     return f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
 }
 template <typename F>
-hts_status by_gradient_shape(int S, F f)
+hts_status by_gradient_lanes(int S, F f)
 {
-    const Shape h = gradient_shape(S);
-    if (h.spt == 4) return f(std::integral_constant<int, 4>(), std::integral_constant<int, 1>());
-    if (h.ls == 1) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
-    if (h.ls == 2) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
-    if (h.ls == 4) return f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
-    return f(std::integral_constant<int, 8>(), std::integral_constant<int, 8>());
+    switch (gradient_lanes(S)) {
+    case 2: return f(std::integral_constant<int, 2>());
+    case 4: return f(std::integral_constant<int, 4>());
+    case 8: return f(std::integral_constant<int, 8>());
+    default: return f(std::integral_constant<int, 16>());
+    }
 }
 
 // Runs so that `blocks` blocks exist, of `least` steps at least and a multiple of the steps staged at once.
@@ -737,7 +760,6 @@ void cut_runs(int T, int64_t base, int64_t blocks, int least, int* runs, int* le
 int64_t channel_blocks(int D, Shape h) { return ceil_div(D, kThreads / h.ls); }
 
 struct Plan {
-    Shape shape;
     int64_t across;
     int runs, length, chunks;
     size_t ends, sums, back, broken, checks, part_bc, part_ch, bytes;           // offsets in the workspace
@@ -745,8 +767,8 @@ struct Plan {
 Plan plan(int T, int N, int D, int S, bool gradient)
 {
     Plan q{};
-    q.shape = gradient ? gradient_shape(S) : scan_shape(S);
-    q.across = channel_blocks(D, q.shape);
+    const int ls = gradient_lanes(S);
+    q.across = gradient ? ceil_div(D, 2 * kThreads / ls) : channel_blocks(D, scan_shape(S));
     cut_runs(T, q.across * N, (int64_t)kCoreSms * (gradient ? 4 : 6), gradient ? 4 * kChunk : 4 * kGroup, &q.runs, &q.length);
     size_t at = 0;
     auto take = [&](size_t floats) { const size_t was = at; at += round256(floats * 4); return was; };
@@ -759,8 +781,8 @@ Plan plan(int T, int N, int D, int S, bool gradient)
     }
     if (gradient) {
         q.chunks = (q.length + kChunk - 1) / kChunk;
-        q.checks = take((size_t)q.runs * N * q.across * q.chunks * q.shape.spt * kThreads);
-        q.part_bc = take((size_t)q.across * T * N * 2 * q.shape.spt * q.shape.ls);
+        q.checks = take((size_t)q.runs * N * q.across * q.chunks * 8 * kThreads);
+        q.part_bc = take((size_t)q.across * T * N * 8 * ls);
         q.part_ch = take((size_t)q.runs * N * ((size_t)D * S + 2 * D));
     }
     q.bytes = at;
@@ -875,18 +897,18 @@ hts_status gradient(ScanArgs p, const hts_scan_inputs& in, const T* dy, int64_t 
         g.first = m.ends;
         g.incoming = m.back;
     }
-    hts_status st = by_gradient_shape(p.S, [&](auto spt, auto ls) {
-        constexpr int SPT = decltype(spt)::value, LS = decltype(ls)::value;
+    hts_status st = by_gradient_lanes(p.S, [&](auto ls) {
+        constexpr int LS = decltype(ls)::value;
         static OncePerDevice allowed[2];
-        auto kernel = wide ? scan_gradient_kernel<T, SPT, LS, true> : scan_gradient_kernel<T, SPT, LS, false>;
+        auto kernel = wide ? scan_gradient_kernel<T, LS, true> : scan_gradient_kernel<T, LS, false>;
         HTS_CUDA(allow_shared(kernel, allowed[wide]));
-        HTS_CUDA(launch_pdl(kernel, dim3(row * q.runs), dim3(kThreads), gradient_shared<T, SPT, LS>(), s, p, g, x, dt, b, c, z, dy, (T*)out.x, (T*)out.dt, (T*)out.z));
+        HTS_CUDA(launch_pdl(kernel, dim3(row * q.runs), dim3(kThreads), sizeof(GradientShared<T, LS>), s, p, g, x, dt, b, c, z, dy, (T*)out.x, (T*)out.dt, (T*)out.z));
         note_launch();
         return HTS_OK;
     });
     if (st != HTS_OK) return st;
     if (out.b || out.c) {
-        const int sp = q.shape.spt * q.shape.ls;
+        const int sp = 4 * gradient_lanes(p.S);
         const int64_t blocks = ceil_div((int64_t)p.T * p.N * 2 * sp, 256);
         HTS_CUDA(launch_pdl(bc_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, s, p, sp, (int)q.across, (const float*)g.part_bc, (T*)out.b, (T*)out.c, out.ld_b, out.ld_c));
         note_launch();
@@ -896,16 +918,25 @@ hts_status gradient(ScanArgs p, const hts_scan_inputs& in, const T* dy, int64_t 
     return launch_column_sums({g.part_ch, (int64_t)q.runs * p.N, states + 2 * p.D, states, states, 1, out.a, out.d, states + p.D, out.dt_bias}, s);
 }
 
+// Elements of the rows of one step, padding between them included: eight steps' offsets fit 32 bits.
+constexpr int64_t kMostInStep = (int64_t)1 << 28;
+bool far(int64_t N, std::initializer_list<int64_t> strides)
+{
+    for (int64_t l : strides)
+        if (l >= kMostInStep || N * l >= kMostInStep) return true;
+    return false;
+}
 // Blocks of one launch, of every kind: a grid has fewer than 2^31.
 bool too_many(int64_t T, int64_t N, int64_t D)
 {
-    return T * N > ((int64_t)1 << 31) || N * D > ((int64_t)1 << 31) || ceil_div(D, 16) * N * ceil_div(T, 32) > INT32_MAX;
+    return T * N > ((int64_t)1 << 31) || N * D >= kMostInStep || N >= kMostInStep / 128 || ceil_div(D, 16) * N * ceil_div(T, 32) > INT32_MAX;
 }
 bool bad(const hts_scan_desc* d, const hts_scan_inputs* in, bool with_steps)
 {
     return !d || !in || (with_steps && d->T < 1) || d->N < 1 || d->channels < 1 || d->state < 1 || d->state > 64 ||
            (d->dtype != HTS_DTYPE_FP32 && d->dtype != HTS_DTYPE_BF16) || !in->x || !in->dt || !in->a || !in->b || !in->c || d->ld_x < d->channels ||
-           d->ld_dt < d->channels || d->ld_b < d->state || d->ld_c < d->state || (in->z && d->ld_z < d->channels) || too_many(with_steps ? d->T : 1, d->N, d->channels);
+           d->ld_dt < d->channels || d->ld_b < d->state || d->ld_c < d->state || (in->z && d->ld_z < d->channels) || too_many(with_steps ? d->T : 1, d->N, d->channels) ||
+           far(d->N, {d->ld_x, d->ld_dt, d->ld_b, d->ld_c, in->z ? d->ld_z : 0});
 }
 
 }  // namespace
@@ -922,7 +953,7 @@ extern "C" int64_t hts_selective_scan_workspace(int32_t T, int32_t N, int32_t ch
 extern "C" hts_status hts_selective_scan(const hts_scan_desc* d, const hts_scan_inputs* in, void* y, float* state_out, void* workspace, int64_t workspace_bytes,
                                          void* stream)
 {
-    if (bad(d, in, true) || !y || d->ld_y < d->channels || y == in->x || y == in->dt || y == in->z || (state_out && state_out == in->state_in)) return HTS_ERR_INVALID_ARG;
+    if (bad(d, in, true) || !y || d->ld_y < d->channels || far(d->N, {d->ld_y}) || y == in->x || y == in->dt || y == in->z || (state_out && state_out == in->state_in)) return HTS_ERR_INVALID_ARG;
     const int64_t need = hts_selective_scan_workspace(d->T, d->N, d->channels, d->state, 0);
     if (need && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return HTS_ERR_INVALID_ARG;
     const ScanArgs p = scan_args(*d, *in);
@@ -943,7 +974,7 @@ extern "C" hts_status hts_selective_scan_step(const hts_scan_desc* d, const hts_
 extern "C" hts_status hts_selective_scan_gradient(const hts_scan_desc* d, const hts_scan_inputs* in, const void* dy, int64_t ld_dy, const float* dstate_out,
                                                   const hts_scan_grads* out, void* workspace, int64_t workspace_bytes, void* stream)
 {
-    if (bad(d, in, true) || !dy || ld_dy < d->channels || !out || (out->x && out->ld_x < d->channels) || (out->dt && out->ld_dt < d->channels) ||
+    if (bad(d, in, true) || !dy || ld_dy < d->channels || !out || far(d->N, {ld_dy, out->x ? out->ld_x : 0, out->dt ? out->ld_dt : 0, out->z ? out->ld_z : 0}) || (out->x && out->ld_x < d->channels) || (out->dt && out->ld_dt < d->channels) ||
         (out->z && (out->ld_z < d->channels || !in->z)) || (out->b && out->ld_b < d->state) || (out->c && out->ld_c < d->state))
         return HTS_ERR_INVALID_ARG;
     if (!out->x && !out->dt && !out->a && !out->b && !out->c && !out->d && !out->dt_bias && !out->z && !out->state_in) return HTS_ERR_INVALID_ARG;
