@@ -247,9 +247,8 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const ConvArgs p, const 
 {
     pdl_wait();
     pdl_trigger();
-    const int64_t id = (int64_t)blockIdx.x * 128 + threadIdx.x;
-    if (id >= (int64_t)p.N * p.lanes) return;
-    const int n = (int)(id / p.lanes), c = (int)(id % p.lanes) * V;
+    const int across = (p.lanes + 127) / 128, lane = (int)(blockIdx.x % across) * 128 + threadIdx.x, n = blockIdx.x / across, c = lane * V;
+    if (lane >= p.lanes) return;
     const int slot = slots ? slots[n] : n;
     if (slot < 0 || slot >= pool) return;
     Vec<T, V> old[W - 1], now = load_vec<V>(x + (size_t)n * p.ld_x + c);
@@ -520,7 +519,7 @@ hts_status step(ConvArgs p, int width, const T* x, const int32_t* slots, int poo
 {
     const bool wide = vectors(p.D, kVector * sizeof(T), {x, win, y, wout}, {p.ld_x, p.ld_y});
     p.lanes = p.D / (wide ? kVector : 1);
-    const int64_t blocks = ceil_div((int64_t)p.N * p.lanes, 128);
+    const int64_t blocks = p.N * ceil_div(p.lanes, 128);
     if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
     return by_width(width, [&](auto k) {
         constexpr int W = decltype(k)::value;

@@ -321,11 +321,10 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const ScanArgs p, const 
 {
     pdl_wait();
     pdl_trigger();
-    const int64_t id = (int64_t)blockIdx.x * 128 + threadIdx.x;
-    const int sub = (int)(id % LS), s0 = sub * 4;
-    const int64_t cn = id / LS, groups = (p.N + ROWS - 1) / ROWS;
-    const bool on = cn < p.D * groups;
-    const int ch = on ? (int)(cn % p.D) : 0, n0 = on ? (int)(cn / p.D) * ROWS : 0;
+    const int across = (p.D * LS + 127) / 128, at0 = (int)(blockIdx.x % across) * 128 + threadIdx.x;
+    const int sub = at0 % LS, s0 = sub * 4, n0 = (int)(blockIdx.x / across) * ROWS;
+    const bool on = at0 / LS < p.D;
+    const int ch = on ? at0 / LS : 0;
     float a2[4];
     if (QUADS) {
         const float4 v = s0 < p.S ? *reinterpret_cast<const float4*>(p.a + (size_t)ch * p.S + s0) : make_float4(0, 0, 0, 0);
@@ -336,55 +335,63 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const ScanArgs p, const 
 #pragma unroll
     for (int i = 0; i < 4; ++i) a2[i] *= kLog2e;
     const float skip = p.d ? p.d[ch] : 0.f, bias = p.dt_bias ? p.dt_bias[ch] : 0.f;
+    // everything that the rows need, asked for before any of it is used
     float h[ROWS][4];
     int slot[ROWS];
+    Vec<T, 4> rb[ROWS], rc[ROWS];
+    T rx[ROWS], rdt[ROWS], rz[ROWS];
+    bool fresh[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         const int n = n0 + r;
         slot[r] = on && n < p.N ? (slots ? slots[n] : n) : -1;
         if (slot[r] >= pool) slot[r] = -1;
-        const size_t at = ((size_t)max(slot[r], 0) * p.D + ch) * p.S + s0;
-        if (QUADS) {
-            const float4 v = slot[r] >= 0 && s0 < p.S ? *reinterpret_cast<const float4*>(state_in + at) : make_float4(0, 0, 0, 0);
-            h[r][0] = v.x; h[r][1] = v.y; h[r][2] = v.z; h[r][3] = v.w;
-        } else
-#pragma unroll
-            for (int i = 0; i < 4; ++i) h[r][i] = slot[r] >= 0 && s0 + i < p.S ? state_in[at + i] : 0.f;
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
+        const float* from = state_in + ((size_t)max(slot[r], 0) * p.D + ch) * p.S + s0;
         const int n = min(n0 + r, p.N - 1);
-        const bool fresh = p.starts && p.starts[n];
-        const float xv = to_float(x[(size_t)n * p.ld_x + ch]), raw = to_float(dt[(size_t)n * p.ld_dt + ch]) + bias, delta = p.softplus ? softplus(raw) : raw;
-        float v = 0.f, bv[4], cv[4];
         if (QUADS) {
-            const Vec<T, 4> rb = load_vec<4>(b + (size_t)n * p.ld_b + (s0 < p.S ? s0 : 0)), rc = load_vec<4>(c + (size_t)n * p.ld_c + (s0 < p.S ? s0 : 0));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { bv[i] = to_float(rb.v[i]); cv[i] = s0 < p.S ? to_float(rc.v[i]) : 0.f; }
+            const float4 v = slot[r] >= 0 && s0 < p.S ? *reinterpret_cast<const float4*>(from) : make_float4(0, 0, 0, 0);
+            h[r][0] = v.x; h[r][1] = v.y; h[r][2] = v.z; h[r][3] = v.w;
+            rb[r] = load_vec<4>(b + (int64_t)n * p.ld_b + (s0 < p.S ? s0 : 0));
+            rc[r] = load_vec<4>(c + (int64_t)n * p.ld_c + (s0 < p.S ? s0 : 0));
         } else
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                bv[i] = s0 + i < p.S ? to_float(b[(size_t)n * p.ld_b + s0 + i]) : 0.f;
-                cv[i] = s0 + i < p.S ? to_float(c[(size_t)n * p.ld_c + s0 + i]) : 0.f;
+                const bool in = s0 + i < p.S;
+                h[r][i] = slot[r] >= 0 && in ? from[i] : 0.f;
+                rb[r].v[i] = in ? (b + (int64_t)n * p.ld_b)[s0 + i] : from_float<T>(0.f);
+                rc[r].v[i] = in ? (c + (int64_t)n * p.ld_c)[s0 + i] : from_float<T>(0.f);
             }
+        rx[r] = (x + (int64_t)n * p.ld_x)[ch];
+        rdt[r] = (dt + (int64_t)n * p.ld_dt)[ch];
+        if (z) rz[r] = (z + (int64_t)n * p.ld_z)[ch];
+        fresh[r] = p.starts && p.starts[n];
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const float xv = to_float(rx[r]), raw = to_float(rdt[r]) + bias, delta = p.softplus ? softplus(raw) : raw;
+        float v = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            h[r][i] = fmaf(exp2_approx(delta * a2[i]), fresh ? 0.f : h[r][i], delta * xv * bv[i]);
-            v = fmaf(cv[i], h[r][i], v);
+            h[r][i] = fmaf(exp2_approx(delta * a2[i]), fresh[r] ? 0.f : h[r][i], delta * xv * to_float(rb[r].v[i]));
+            v = s0 + i < p.S ? fmaf(to_float(rc[r].v[i]), h[r][i], v) : v;
         }
 #pragma unroll
         for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         v = fmaf(skip, xv, v);
-        if (z) v *= silu(to_float(z[(size_t)n * p.ld_z + ch]));
+        if (z) v *= silu(to_float(rz[r]));
         if (slot[r] < 0) continue;
-        if (sub == 0) y[(size_t)n * p.ld_y + ch] = from_float<T>(v);
-        const size_t at = ((size_t)slot[r] * p.D + ch) * p.S + s0;
+        const int n = n0 + r;
+        if (sub == 0) (y + (int64_t)n * p.ld_y)[ch] = from_float<T>(v);
+        float* to = state_out + ((size_t)slot[r] * p.D + ch) * p.S + s0;
         if (QUADS) {
-            if (s0 < p.S) *reinterpret_cast<float4*>(state_out + at) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
+            if (s0 < p.S) *reinterpret_cast<float4*>(to) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
         } else
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (s0 + i < p.S) state_out[at + i] = h[r][i];
+                if (s0 + i < p.S) to[i] = h[r][i];
     }
 }
 
@@ -398,7 +405,7 @@ struct GradArgs {
     float *dstate_in;
     int chunks;                                 // of kChunk steps, per run
 };
-constexpr int kChunk = 8;
+constexpr int kChunk = 8, kKept = 4;              // steps of a chunk; steps whose states a thread keeps at a time
 template <int LS> struct GradientShape {
     static constexpr int SP = 4 * LS, CB = 2 * kThreads / LS;                   // states with the padding, channels of a block
 };
@@ -418,9 +425,11 @@ template <typename T, int LS> struct GradientShared {
 // channel) crosses LS lanes, what has to be added over channels (dB and dC, eight sums, two channels of which meet in the thread)
 // the others: in the first exchanges of each each lane keeps half of the sums and hands on the other half.  With eight states of one
 // channel in a thread, states and gradients in shared memory and the sums over channels read from there, shared memory
-// bounded it (105 accesses a warp and step): 1165 us for 128 x 256 steps of 1024 channels and 16 states, now @G.
+// bounded it (105 accesses a warp and step): 1165 us for 128 x 256 steps of 1024 channels and 16 states, as long as this takes (1135),
+// which has 42 % of the accesses and is bound by latency: three warps a scheduler of 160 registers, 0.53 instructions a clock.  Four
+// with states of two steps (1201) or chunks of four (1077, but twice the memory for checks) do not change that much.
 template <typename T, int LS, bool WIDE>
-__global__ void __launch_bounds__(kThreads, VGB) scan_gradient_kernel(const ScanArgs p, const GradArgs q, const T* x, const T* dt, const T* b, const T* c, const T* z,
+__global__ void __launch_bounds__(kThreads, 3) scan_gradient_kernel(const ScanArgs p, const GradArgs q, const T* x, const T* dt, const T* b, const T* c, const T* z,
                                                                     const T* dy, T* dx, T* ddt, T* dz)
 {
     using S = GradientShape<LS>;
@@ -569,17 +578,17 @@ __global__ void __launch_bounds__(kThreads, VGB) scan_gradient_kernel(const Scan
         // half a chunk at a time, so that its states fit the registers beside the rest
         by_starts([&](auto with_starts) {
 #pragma unroll 1
-            for (int from = kChunk / 2; from >= 0; from -= kChunk / 2) {
-            f32x2 before[2][2], h[kChunk / 2][2][2];
+            for (int from = kChunk - kKept; from >= 0; from -= kKept) {
+            f32x2 before[2][2], h[kKept][2][2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) { before[e][0] = h0[e][0]; before[e][1] = h0[e][1]; }
-            if (from)
+            if (kChunk > kKept && from)
 #pragma unroll
-                for (int j = 0; j < kChunk / 2; ++j) advance(with_starts, j, before, before);
+                for (int j = 0; j < kKept; ++j) advance(with_starts, j, before, before);
 #pragma unroll
-            for (int i = 0; i < kChunk / 2; ++i) advance(with_starts, from + i, i ? h[i - 1] : before, h[i]);
+            for (int i = 0; i < kKept; ++i) advance(with_starts, from + i, i ? h[i - 1] : before, h[i]);
 #pragma unroll
-            for (int at = kChunk / 2 - 1; at >= 0; --at) {                      // back over its steps
+            for (int at = kKept - 1; at >= 0; --at) {                      // back over its steps
                 const int j = from + at;
                 const float4 du = sh.du[j][pc];
                 const float2 gv = *reinterpret_cast<const float2*>(&sh.g[j][2 * pc]);
@@ -852,12 +861,12 @@ hts_status step(const ScanArgs& p, const hts_scan_inputs& in, const int32_t* slo
                        aligned_to(in.c, 4 * sizeof(T)) && p.ld_b % 4 == 0 && p.ld_c % 4 == 0;
     const T *x = (const T*)in.x, *dt = (const T*)in.dt, *b = (const T*)in.b, *c = (const T*)in.c, *z = (const T*)in.z;
     auto go = [&](auto ls) {
-        constexpr int LS = decltype(ls)::value;
-        // four rows a thread where that leaves eight blocks on every SM
-        const bool many = (int64_t)p.N * p.D * LS / 4 >= (int64_t)kCoreSms * 1024;
-        const int64_t blocks = ceil_div((int64_t)(many ? (p.N + 3) / 4 : p.N) * p.D * LS, 128);
-        if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
-        auto kernel = many ? (quads ? scan_step_kernel<T, LS, true, 4> : scan_step_kernel<T, LS, false, 4>)
+        constexpr int LS = decltype(ls)::value, ROWS = 2;
+        // two rows a thread where that leaves eight blocks on every SM: 1024 rows of 1024 channels 37 us, with one 40, with four 46
+        const bool many = (int64_t)p.N * p.D * LS / ROWS >= (int64_t)kCoreSms * 1024;
+        const int64_t blocks = (int64_t)(many ? (p.N + ROWS - 1) / ROWS : p.N) * ceil_div((int64_t)p.D * LS, 128);
+        if (blocks > INT32_MAX || (int64_t)p.D * LS > INT32_MAX - 128) return HTS_ERR_INVALID_ARG;
+        auto kernel = many ? (quads ? scan_step_kernel<T, LS, true, ROWS> : scan_step_kernel<T, LS, false, ROWS>)
                            : (quads ? scan_step_kernel<T, LS, true, 1> : scan_step_kernel<T, LS, false, 1>);
         HTS_CUDA(launch_pdl(kernel, dim3((unsigned)blocks), dim3(128), 0, s, p, x, dt, b, c, z, slots, pool, in.state_in, y, state_out));
         note_launch();
