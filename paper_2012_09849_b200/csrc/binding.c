@@ -168,7 +168,17 @@ static int look(PyObject *x, const char *name, int want, Seen *v)
     if (!ok) return PyErr_Occurred() ? 0 : refuse(PyExc_ValueError, name, "has the wrong shape");
     return int_ptr(PyObject_CallMethodNoArgs(x, s_data_ptr), &v->ptr);
 }
-/* memory of the current CUDA device */
+/* memory of the CUDA device that was current when the call began (began()) */
+static long g_current;
+static int began(void)
+{
+    if (!torch_types()) return 0;
+    PyObject *cur = PyObject_CallNoArgs(g_get_device);
+    g_current = cur ? PyLong_AsLong(cur) : -1;
+    if (!cur) PyErr_Clear();                           /* no device: no tensor of one either */
+    Py_XDECREF(cur);
+    return 1;
+}
 static int here(PyObject *x, const char *name)
 {
     PyObject *at = PyObject_CallMethodNoArgs(x, s_get_device);
@@ -176,47 +186,47 @@ static int here(PyObject *x, const char *name)
     Py_XDECREF(at);
     if (!at || (d == -1 && PyErr_Occurred())) return 0;
     if (d < 0) return refuse(PyExc_ValueError, name, "is not on a CUDA device");
-    PyObject *cur = PyObject_CallNoArgs(g_get_device);
-    const long c = cur ? PyLong_AsLong(cur) : -1;
-    Py_XDECREF(cur);
-    if (!cur || (c == -1 && PyErr_Occurred())) return 0;
-    return c == d || refuse(PyExc_ValueError, name, "is not on the current device");
+    return g_current == d || refuse(PyExc_ValueError, name, "is not on the current device");
 }
-/* Rows: [d0, cols], or [d0, d1, cols] with d1 > 0, the rows evenly spaced and their elements adjacent.  None is NULL. */
-static int to_rows(PyObject *x, const char *name, int64_t d0, int64_t d1, int64_t cols, int type, void **ptr, int64_t *ld)
+/* Rows: [d0, cols], or [d0, d1, cols] with d1 > 0, the rows evenly spaced and their elements adjacent. */
+static int rows_of(const Seen *v, PyObject *x, const char *name, int64_t d0, int64_t d1, int64_t cols, void **ptr, int64_t *ld)
 {
-    *ptr = NULL; *ld = 0;
-    if (x == Py_None) return 1;
-    Seen v;
     const int lead = d1 > 0 ? 2 : 1;
-    if (!look(x, name, type, &v)) return 0;
-    if (v.dims != lead + 1 || v.size[0] != d0 || (lead == 2 && v.size[1] != d1) || v.size[lead] != cols) return refuse(PyExc_ValueError, name, "has the wrong shape");
-    int ok = cols == 1 || v.stride[lead] == 1;
-    if (lead == 2 && d1 > 1) { *ld = v.stride[1]; ok = ok && (d0 == 1 || v.stride[0] == d1 * *ld); }
-    else *ld = d0 > 1 ? v.stride[0] : cols;
+    if (v->dims != lead + 1 || v->size[0] != d0 || (lead == 2 && v->size[1] != d1) || v->size[lead] != cols) return refuse(PyExc_ValueError, name, "has the wrong shape");
+    int ok = cols == 1 || v->stride[lead] == 1;
+    if (lead == 2 && d1 > 1) { *ld = v->stride[1]; ok = ok && (d0 == 1 || v->stride[0] == d1 * *ld); }
+    else *ld = d0 > 1 ? v->stride[0] : cols;
     if (!ok || *ld < cols) return refuse(PyExc_ValueError, name, "needs evenly spaced rows of adjacent elements");
-    *ptr = v.ptr;
+    *ptr = v->ptr;
     return here(x, name);
 }
-/* A dense tensor of the given sizes (0 ends them).  None is NULL. */
-static int to_dense(PyObject *x, const char *name, int type, int64_t a, int64_t b, int64_t c, void **ptr)
+static int to_rows(PyObject *x, const char *name, int64_t d0, int64_t d1, int64_t cols, int type, void **ptr, int64_t *ld)      /* None is NULL */
 {
-    *ptr = NULL;
-    if (x == Py_None) return 1;
     Seen v;
+    *ptr = NULL; *ld = 0;
+    return x == Py_None || (look(x, name, type, &v) && rows_of(&v, x, name, d0, d1, cols, ptr, ld));
+}
+/* A dense tensor of the given sizes (0 ends them). */
+static int dense_of(const Seen *v, PyObject *x, const char *name, int64_t a, int64_t b, int64_t c, void **ptr)
+{
     const int64_t want[3] = {a, b, c};
     const int dims = c ? 3 : b ? 2 : 1;
-    if (!look(x, name, type, &v)) return 0;
-    int ok = v.dims == dims;
-    for (int i = 0; ok && i < dims; ++i) ok = v.size[i] == want[i];
+    int ok = v->dims == dims;
+    for (int i = 0; ok && i < dims; ++i) ok = v->size[i] == want[i];
     if (!ok) return refuse(PyExc_ValueError, name, "has the wrong shape");
     int64_t dense = 1;
     for (int i = dims - 1; i >= 0; --i) {
-        if (v.size[i] > 1 && v.stride[i] != dense) return refuse(PyExc_ValueError, name, "must be contiguous");
-        dense *= v.size[i];
+        if (v->size[i] > 1 && v->stride[i] != dense) return refuse(PyExc_ValueError, name, "must be contiguous");
+        dense *= v->size[i];
     }
-    *ptr = v.ptr;
+    *ptr = v->ptr;
     return here(x, name);
+}
+static int to_dense(PyObject *x, const char *name, int type, int64_t a, int64_t b, int64_t c, void **ptr)                       /* None is NULL */
+{
+    Seen v;
+    *ptr = NULL;
+    return x == Py_None || (look(x, name, type, &v) && dense_of(&v, x, name, a, b, c, ptr));
 }
 /* Device memory of any type: its address and bytes.  None is NULL. */
 static int to_workspace(PyObject *x, void **ptr, int64_t *bytes)
@@ -230,25 +240,13 @@ static int to_workspace(PyObject *x, void **ptr, int64_t *bytes)
     Py_XDECREF(n);
     return *bytes >= 0 && to_ptr(x, ptr) && here(x, "workspace");
 }
-/* [N, width], or [T, N, width]: the tensor that the others follow */
-static int to_lead(PyObject *x, const char *name, int lead, int32_t *dtype, int64_t *T, int64_t *N, int64_t *width)
+/* A tensor of `dims` dimensions, each a positive 32-bit number: one that the others follow. */
+static int to_lead(PyObject *x, const char *name, int type, int dims, Seen *v)
 {
-    Seen v;
-    if (!look(x, name, -1, &v)) return 0;
-    if (v.dims != lead + 1) return refuse(PyExc_ValueError, name, "has the wrong shape");
-    for (int i = 0; i < v.dims; ++i)
-        if (v.size[i] < 1 || v.size[i] > INT32_MAX) return refuse(PyExc_ValueError, name, "has the wrong shape");
-    *dtype = v.type; *T = lead == 2 ? v.size[0] : 0; *N = v.size[lead - 1]; *width = v.size[lead];
-    return 1;
-}
-/* the size of a tensor's dimension i, of `dims` */
-static int to_size(PyObject *x, const char *name, int type, int dims, int i, int64_t *out)
-{
-    Seen v;
-    if (!look(x, name, type, &v)) return 0;
-    if (v.dims != dims || v.size[i] < 1 || v.size[i] > INT32_MAX) return refuse(PyExc_ValueError, name, "has the wrong shape");
-    *out = v.size[i];
-    return 1;
+    if (!look(x, name, type, v)) return 0;
+    int ok = v->dims == dims;
+    for (int i = 0; ok && i < dims; ++i) ok = v->size[i] >= 1 && v->size[i] <= INT32_MAX;
+    return ok || refuse(PyExc_ValueError, name, "has the wrong shape");
 }
 static PyObject *entry(PyObject *dict, const char *key)                 /* borrowed; None if there is no such key */
 {
@@ -388,16 +386,20 @@ static PyObject *conv_like(PyObject *const *a, Py_ssize_t nargs, int form)      
     float *w, *bias, *dwout = NULL, *dw = NULL, *db = NULL, *dwin = NULL;
     uint8_t *starts;
     int32_t *index;
-    if (!to_lead(a[0], "x", lead, &dtype, &T, &N, &D) || !to_size(a[1], "w", F32_T, 2, 1, &W)) return NULL;
+    Seen vx, vw, vp;
+    if (!began() || !to_lead(a[0], "x", -1, lead + 1, &vx) || !to_lead(a[1], "w", F32_T, 2, &vw)) return NULL;
+    dtype = vx.type; T = lead == 2 ? vx.size[0] : 0; N = vx.size[lead - 1]; D = vx.size[lead]; W = vw.size[1];
     if (W < 2 || W > 4) { refuse(PyExc_ValueError, "w", "needs two to four taps"); return NULL; }
     const int64_t d0 = lead == 2 ? T : N, d1 = lead == 2 ? N : 0;
-    ROWS(a[0], "x", d0, d1, D, x, d.ld_x);
-    DENSE(a[1], "w", F32_T, D, W, 0, w);
+    if (!rows_of(&vx, a[0], "x", d0, d1, D, &x, &d.ld_x) || !dense_of(&vw, a[1], "w", D, W, 0, (void **)&w)) return NULL;
     DENSE(a[2], "bias", F32_T, D, 0, 0, bias);
     DENSE(a[3], "starts", U8_T, d0, d1, 0, starts);
     DENSE(a[4], form == 1 ? "slots" : "lengths", I32_T, N, 0, 0, index);
-    if (form == 1 && !to_size(a[5], "window_in", dtype, 3, 0, &pool)) return NULL;
-    DENSE(a[5], "window_in", dtype, form == 1 ? pool : N, W - 1, D, win);
+    if (form == 1) {
+        if (!to_lead(a[5], "window_in", dtype, 3, &vp) || !dense_of(&vp, a[5], "window_in", vp.size[0], W - 1, D, &win)) return NULL;
+        pool = vp.size[0];
+    } else
+        DENSE(a[5], "window_in", dtype, N, W - 1, D, win);
     I32(act, 6);
     d.T = (int32_t)T; d.N = (int32_t)N; d.channels = (int32_t)D; d.width = (int32_t)W; d.dtype = dtype; d.activation = act;
     if (form == 2) {
@@ -433,11 +435,12 @@ static PyObject *scan_like(PyObject *const *a, Py_ssize_t nargs, int form)
     void *y = NULL, *dy = NULL, *work = NULL;
     float *sout = NULL, *dsout = NULL;
     int32_t *index;
-    if (!to_lead(a[0], "x", lead, &dtype, &T, &N, &D) || !to_size(a[2], "a", F32_T, 2, 1, &S)) return NULL;
+    Seen vx, va, vp;
+    if (!began() || !to_lead(a[0], "x", -1, lead + 1, &vx) || !to_lead(a[2], "a", F32_T, 2, &va)) return NULL;
+    dtype = vx.type; T = lead == 2 ? vx.size[0] : 0; N = vx.size[lead - 1]; D = vx.size[lead]; S = va.size[1];
     const int64_t d0 = lead == 2 ? T : N, d1 = lead == 2 ? N : 0;
-    ROWS(a[0], "x", d0, d1, D, in.x, d.ld_x);
+    if (!rows_of(&vx, a[0], "x", d0, d1, D, (void **)&in.x, &d.ld_x) || !dense_of(&va, a[2], "a", D, S, 0, (void **)&in.a)) return NULL;
     ROWS(a[1], "dt", d0, d1, D, in.dt, d.ld_dt);
-    DENSE(a[2], "a", F32_T, D, S, 0, in.a);
     ROWS(a[3], "b", d0, d1, S, in.b, d.ld_b);
     ROWS(a[4], "c", d0, d1, S, in.c, d.ld_c);
     DENSE(a[5], "d", F32_T, D, 0, 0, in.d);
@@ -445,8 +448,11 @@ static PyObject *scan_like(PyObject *const *a, Py_ssize_t nargs, int form)
     ROWS(a[7], "z", d0, d1, D, in.z, d.ld_z);
     DENSE(a[8], "starts", U8_T, d0, d1, 0, in.starts);
     DENSE(a[9], form == 1 ? "slots" : "lengths", I32_T, N, 0, 0, index);
-    if (form == 1 && !to_size(a[10], "state_in", F32_T, 3, 0, &pool)) return NULL;
-    DENSE(a[10], "state_in", F32_T, form == 1 ? pool : N, D, S, in.state_in);
+    if (form == 1) {
+        if (!to_lead(a[10], "state_in", F32_T, 3, &vp) || !dense_of(&vp, a[10], "state_in", vp.size[0], D, S, (void **)&in.state_in)) return NULL;
+        pool = vp.size[0];
+    } else
+        DENSE(a[10], "state_in", F32_T, N, D, S, in.state_in);
     const int soft = PyObject_IsTrue(a[11]);
     if (soft < 0) return NULL;
     d.T = (int32_t)T; d.N = (int32_t)N; d.channels = (int32_t)D; d.state = (int32_t)S; d.dtype = dtype; d.softplus = soft;
@@ -486,15 +492,15 @@ FN(linear)
 {
     (void)self;
     ARGS(9);
-    int32_t dtype;
-    int64_t T, M, K, N, bytes;
+    int64_t M, K, N, bytes;
+    Seen vx, vw;
     hts_linear_desc d = {0};
     void *x, *w, *res, *y, *pre, *work;
     float *bias;
-    if (!to_lead(a[0], "x", 1, &dtype, &T, &M, &K) || !to_size(a[1], "w", BF16_T, 2, 0, &N)) return NULL;
-    dtype = BF16_T;
-    ROWS(a[0], "x", M, 0, K, x, d.ld_x);
-    DENSE(a[1], "w", BF16_T, N, K, 0, w);
+    const int32_t dtype = BF16_T;
+    if (!began() || !to_lead(a[0], "x", dtype, 2, &vx) || !to_lead(a[1], "w", dtype, 2, &vw)) return NULL;
+    M = vx.size[0]; K = vx.size[1]; N = vw.size[0];
+    if (!rows_of(&vx, a[0], "x", M, 0, K, &x, &d.ld_x) || !dense_of(&vw, a[1], "w", N, K, 0, &w)) return NULL;
     DENSE(a[2], "bias", F32_T, N, 0, 0, bias);
     ROWS(a[3], "residual", M, 0, N, res, d.ld_residual);
     I32(act, 4);
@@ -509,15 +515,15 @@ FN(linear_gradient)
 {
     (void)self;
     ARGS(10);
-    int32_t dtype;
-    int64_t T, M, K, N, bytes;
+    int64_t M, K, N, bytes;
+    Seen vx, vw;
     hts_linear_desc d = {0};
     void *x, *w, *pre, *dy, *dx, *dw = NULL, *work;
     float *db;
-    if (!to_lead(a[0], "x", 1, &dtype, &T, &M, &K) || !to_size(a[1], "w", BF16_T, 2, 0, &N)) return NULL;
-    dtype = BF16_T;
-    ROWS(a[0], "x", M, 0, K, x, d.ld_x);
-    DENSE(a[1], "w", BF16_T, N, K, 0, w);
+    const int32_t dtype = BF16_T;
+    if (!began() || !to_lead(a[0], "x", dtype, 2, &vx) || !to_lead(a[1], "w", dtype, 2, &vw)) return NULL;
+    M = vx.size[0]; K = vx.size[1]; N = vw.size[0];
+    if (!rows_of(&vx, a[0], "x", M, 0, K, &x, &d.ld_x) || !dense_of(&vw, a[1], "w", N, K, 0, &w)) return NULL;
     ROWS(a[2], "pre", M, 0, N, pre, d.ld_pre);
     ROWS(a[3], "dy", M, 0, N, dy, d.ld_dy);
     I32(act, 4);
