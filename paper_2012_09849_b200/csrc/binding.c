@@ -168,11 +168,13 @@ static int look(PyObject *x, const char *name, int want, Seen *v)
     if (!ok) return PyErr_Occurred() ? 0 : refuse(PyExc_ValueError, name, "has the wrong shape");
     return int_ptr(PyObject_CallMethodNoArgs(x, s_data_ptr), &v->ptr);
 }
-/* memory of the CUDA device that was current when the call began (began()) */
+/* memory of the CUDA device that was current when the call began (began()); what is not is reported when all else is right */
 static long g_current;
+static const char *g_elsewhere, *g_where;
 static int began(void)
 {
     if (!torch_types()) return 0;
+    g_elsewhere = NULL;
     PyObject *cur = PyObject_CallNoArgs(g_get_device);
     g_current = cur ? PyLong_AsLong(cur) : -1;
     if (!cur) PyErr_Clear();                           /* no device: no tensor of one either */
@@ -185,8 +187,11 @@ static int here(PyObject *x, const char *name)
     const long d = at ? PyLong_AsLong(at) : -1;
     Py_XDECREF(at);
     if (!at || (d == -1 && PyErr_Occurred())) return 0;
-    if (d < 0) return refuse(PyExc_ValueError, name, "is not on a CUDA device");
-    return g_current == d || refuse(PyExc_ValueError, name, "is not on the current device");
+    if (!g_elsewhere && (d < 0 || d != g_current)) {
+        g_elsewhere = name;
+        g_where = d < 0 ? "is not on a CUDA device" : "is not on the current device";
+    }
+    return 1;
 }
 /* Rows: [d0, cols], or [d0, d1, cols] with d1 > 0, the rows evenly spaced and their elements adjacent. */
 static int rows_of(const Seen *v, PyObject *x, const char *name, int64_t d0, int64_t d1, int64_t cols, void **ptr, int64_t *ld)
@@ -372,6 +377,9 @@ FN(vtrace)
     PTR(vs, 11); PTR(pg, 12); STREAM(13);
     CALL(hts_vtrace(lr, r, v, d, b, gamma, lambda, rho, c, T, N, vs, pg, stream), "hts_vtrace");
 }
+#define CORE_CALL(expr, what) \
+    if (g_elsewhere) { refuse(PyExc_ValueError, g_elsewhere, g_where); return NULL; } \
+    CALL(expr, what)
 #define ROWS(x, name, d0, d1, cols, ptr, ld) if (!to_rows(x, name, d0, d1, cols, dtype, (void **)&(ptr), &(ld))) return NULL
 #define DENSE(x, name, type, d0, d1, d2, ptr) if (!to_dense(x, name, type, d0, d1, d2, (void **)&(ptr))) return NULL
 
@@ -411,13 +419,13 @@ static PyObject *conv_like(PyObject *const *a, Py_ssize_t nargs, int form)      
         DENSE(a[12], "dwindow_in", F32_T, N, W - 1, D, dwin);
         if (!to_workspace(a[13], &work, &bytes)) return NULL;
         STREAM(14);
-        CALL(hts_causal_conv_gradient(&d, x, w, bias, starts, index, win, dy, dwout, dx, dw, db, dwin, work, bytes, stream), "hts_causal_conv_gradient");
+        CORE_CALL(hts_causal_conv_gradient(&d, x, w, bias, starts, index, win, dy, dwout, dx, dw, db, dwin, work, bytes, stream), "hts_causal_conv_gradient");
     }
     ROWS(a[7], "y", d0, d1, D, y, d.ld_y);
     DENSE(a[8], "window_out", dtype, form == 1 ? pool : N, W - 1, D, wout);
     STREAM(9);
-    if (form == 1) { CALL(hts_causal_conv_step(&d, x, w, bias, starts, index, (int32_t)pool, win, y, wout, stream), "hts_causal_conv_step"); }
-    CALL(hts_causal_conv(&d, x, w, bias, starts, index, win, y, wout, stream), "hts_causal_conv");
+    if (form == 1) { CORE_CALL(hts_causal_conv_step(&d, x, w, bias, starts, index, (int32_t)pool, win, y, wout, stream), "hts_causal_conv_step"); }
+    CORE_CALL(hts_causal_conv(&d, x, w, bias, starts, index, win, y, wout, stream), "hts_causal_conv");
 }
 FN(causal_conv) { (void)self; return conv_like(a, nargs, 0); }
 FN(causal_conv_step) { (void)self; return conv_like(a, nargs, 1); }
@@ -472,17 +480,17 @@ static PyObject *scan_like(PyObject *const *a, Py_ssize_t nargs, int form)
         DENSE(entry(a[14], "state_in"), "grads['state_in']", F32_T, N, D, S, g.state_in);
         if (!to_workspace(a[15], &work, &bytes)) return NULL;
         STREAM(16);
-        CALL(hts_selective_scan_gradient(&d, &in, dy, ld_dy, dsout, &g, work, bytes, stream), "hts_selective_scan_gradient");
+        CORE_CALL(hts_selective_scan_gradient(&d, &in, dy, ld_dy, dsout, &g, work, bytes, stream), "hts_selective_scan_gradient");
     }
     ROWS(a[12], "y", d0, d1, D, y, d.ld_y);
     DENSE(a[13], "state_out", F32_T, form == 1 ? pool : N, D, S, sout);
     if (form == 1) {
         STREAM(14);
-        CALL(hts_selective_scan_step(&d, &in, index, (int32_t)pool, y, sout, stream), "hts_selective_scan_step");
+        CORE_CALL(hts_selective_scan_step(&d, &in, index, (int32_t)pool, y, sout, stream), "hts_selective_scan_step");
     }
     if (!to_workspace(a[14], &work, &bytes)) return NULL;
     STREAM(15);
-    CALL(hts_selective_scan(&d, &in, y, sout, work, bytes, stream), "hts_selective_scan");
+    CORE_CALL(hts_selective_scan(&d, &in, y, sout, work, bytes, stream), "hts_selective_scan");
 }
 FN(selective_scan) { (void)self; return scan_like(a, nargs, 0); }
 FN(selective_scan_step) { (void)self; return scan_like(a, nargs, 1); }
@@ -509,7 +517,7 @@ FN(linear)
     if (!to_workspace(a[7], &work, &bytes)) return NULL;
     STREAM(8);
     d.rows = (int32_t)M; d.in_features = (int32_t)K; d.out_features = (int32_t)N; d.activation = act;
-    CALL(hts_linear(&d, x, w, bias, res, y, pre, work, bytes, stream), "hts_linear");
+    CORE_CALL(hts_linear(&d, x, w, bias, res, y, pre, work, bytes, stream), "hts_linear");
 }
 FN(linear_gradient)
 {
@@ -538,7 +546,7 @@ FN(linear_gradient)
     if (!to_workspace(a[8], &work, &bytes)) return NULL;
     STREAM(9);
     d.rows = (int32_t)M; d.in_features = (int32_t)K; d.out_features = (int32_t)N; d.activation = act;
-    CALL(hts_linear_gradient(&d, x, w, pre, dy, dx, dw, db, work, bytes, stream), "hts_linear_gradient");
+    CORE_CALL(hts_linear_gradient(&d, x, w, pre, dy, dx, dw, db, work, bytes, stream), "hts_linear_gradient");
 }
 
 static PyObject *init(PyObject *self, PyObject *error)

@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(256) dz_kernel(const bf16* dy, int64_t ld_dy, 
             if (pre) {
                 const Vec<bf16, V> u = load_vec<V>(pre + row * ld_pre + c);
 #pragma unroll
-                for (int k = 0; k < V; ++k) v[k] *= slope_of(to_float(u.v[k]), act);
+                for (int k = 0; k < V; ++k) v[k] = __fmul_rn(v[k], slope_of(to_float(u.v[k]), act));     // the same whether dz is stored or only added
             }
 #pragma unroll
             for (int k = 0; k < V; ++k) sum[k] += v[k];
