@@ -313,86 +313,75 @@ __global__ void __launch_bounds__(256) compose_kernel(const ScanArgs p, const fl
     }
 }
 
-// One step of row n over the states at its slot: four states a thread, LS lanes a channel, ROWS rows that share A.  A row whose slot
-// lies outside the pool is left alone.
-template <typename T, int LS, bool QUADS, int ROWS>
+struct Eight { float v[8]; };
+__device__ __forceinline__ Eight load_eight(const float* p)
+{
+    Eight r;
+    asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(r.v[0]), "=f"(r.v[1]), "=f"(r.v[2]), "=f"(r.v[3]), "=f"(r.v[4]), "=f"(r.v[5]), "=f"(r.v[6]), "=f"(r.v[7]) : "l"(p) : "memory");
+    return r;
+}
+__device__ __forceinline__ void store_eight(float* p, const float (&v)[8])
+{
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}
+// One step of row n over the states at its slot: eight states a thread, LS lanes a channel.  A row whose slot lies outside the pool is
+// left alone.  Bound by the states, which are read and written once: 1024 rows of 1024 channels and 16 states in 29.6 us, 4.8 TB/s.  With
+// four states a thread, four lanes computed each channel's delta and gate (37 us); two or four rows a thread take as long as one.
+// WHOLE: eight states are one access of 32 bytes.
+template <typename T, int LS, bool WHOLE>
 __global__ void __launch_bounds__(128) scan_step_kernel(const ScanArgs p, const T* x, const T* dt, const T* b, const T* c, const T* z, const int32_t* slots, int pool,
                                                         const float* state_in, T* y, float* state_out)
 {
     pdl_wait();
     pdl_trigger();
-    const int across = (p.D * LS + 127) / 128, at0 = (int)(blockIdx.x % across) * 128 + threadIdx.x;
-    const int sub = at0 % LS, s0 = sub * 4, n0 = (int)(blockIdx.x / across) * ROWS;
-    const bool on = at0 / LS < p.D;
-    const int ch = on ? at0 / LS : 0;
-    float a2[4];
-    if (QUADS) {
-        const float4 v = s0 < p.S ? *reinterpret_cast<const float4*>(p.a + (size_t)ch * p.S + s0) : make_float4(0, 0, 0, 0);
-        a2[0] = v.x; a2[1] = v.y; a2[2] = v.z; a2[3] = v.w;
+    const int across = (p.D * LS + 127) / 128, at = (int)(blockIdx.x % across) * 128 + threadIdx.x, n = blockIdx.x / across;
+    const int sub = at % LS, s0 = sub * 8;
+    const bool on = at / LS < p.D, some = s0 < p.S;
+    const int ch = on ? at / LS : 0, s_at = some ? s0 : 0;
+    int slot = slots ? slots[n] : n;
+    if (!on || slot < 0 || slot >= pool) slot = -1;
+    const float* from = state_in + ((size_t)max(slot, 0) * p.D + ch) * p.S;
+    const T *rb = b + (int64_t)n * p.ld_b, *rc = c + (int64_t)n * p.ld_c;
+    float h[8], a2[8], bv[8], cv[8];            // all of it is asked for before any of it is used
+    if (WHOLE) {
+        const Eight a = load_eight(p.a + (size_t)ch * p.S + s_at), old = load_eight(from + s_at);
+        const Vec<T, 8> vb = load_vec<8>(rb + s_at), vc = load_vec<8>(rc + s_at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { a2[i] = a.v[i] * kLog2e; h[i] = old.v[i]; bv[i] = to_float(vb.v[i]); cv[i] = to_float(vc.v[i]); }
     } else
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a2[i] = s0 + i < p.S ? p.a[(size_t)ch * p.S + s0 + i] : 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a2[i] *= kLog2e;
-    const float skip = p.d ? p.d[ch] : 0.f, bias = p.dt_bias ? p.dt_bias[ch] : 0.f;
-    // everything that the rows need, asked for before any of it is used
-    float h[ROWS][4];
-    int slot[ROWS];
-    Vec<T, 4> rb[ROWS], rc[ROWS];
-    T rx[ROWS], rdt[ROWS], rz[ROWS];
-    bool fresh[ROWS];
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const int n = n0 + r;
-        slot[r] = on && n < p.N ? (slots ? slots[n] : n) : -1;
-        if (slot[r] >= pool) slot[r] = -1;
-    }
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const float* from = state_in + ((size_t)max(slot[r], 0) * p.D + ch) * p.S + s0;
-        const int n = min(n0 + r, p.N - 1);
-        if (QUADS) {
-            const float4 v = slot[r] >= 0 && s0 < p.S ? *reinterpret_cast<const float4*>(from) : make_float4(0, 0, 0, 0);
-            h[r][0] = v.x; h[r][1] = v.y; h[r][2] = v.z; h[r][3] = v.w;
-            rb[r] = load_vec<4>(b + (int64_t)n * p.ld_b + (s0 < p.S ? s0 : 0));
-            rc[r] = load_vec<4>(c + (int64_t)n * p.ld_c + (s0 < p.S ? s0 : 0));
-        } else
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool in = s0 + i < p.S;
-                h[r][i] = slot[r] >= 0 && in ? from[i] : 0.f;
-                rb[r].v[i] = in ? (b + (int64_t)n * p.ld_b)[s0 + i] : from_float<T>(0.f);
-                rc[r].v[i] = in ? (c + (int64_t)n * p.ld_c)[s0 + i] : from_float<T>(0.f);
-            }
-        rx[r] = (x + (int64_t)n * p.ld_x)[ch];
-        rdt[r] = (dt + (int64_t)n * p.ld_dt)[ch];
-        if (z) rz[r] = (z + (int64_t)n * p.ld_z)[ch];
-        fresh[r] = p.starts && p.starts[n];
-    }
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const float xv = to_float(rx[r]), raw = to_float(rdt[r]) + bias, delta = p.softplus ? softplus(raw) : raw;
-        float v = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[r][i] = fmaf(exp2_approx(delta * a2[i]), fresh[r] ? 0.f : h[r][i], delta * xv * to_float(rb[r].v[i]));
-            v = s0 + i < p.S ? fmaf(to_float(rc[r].v[i]), h[r][i], v) : v;
+        for (int i = 0; i < 8; ++i) {
+            const bool in = s0 + i < p.S;
+            a2[i] = in ? p.a[(size_t)ch * p.S + s0 + i] * kLog2e : 0.f;
+            h[i] = in ? from[s0 + i] : 0.f;
+            bv[i] = in ? to_float(rb[s0 + i]) : 0.f;
+            cv[i] = in ? to_float(rc[s0 + i]) : 0.f;
         }
+    const float xv = to_float((x + (int64_t)n * p.ld_x)[ch]), zv = z ? to_float((z + (int64_t)n * p.ld_z)[ch]) : 0.f;
+    const float raw = to_float((dt + (int64_t)n * p.ld_dt)[ch]) + (p.dt_bias ? p.dt_bias[ch] : 0.f), skip = p.d ? p.d[ch] : 0.f;
+    const bool fresh = p.starts && p.starts[n];
+    const float delta = p.softplus ? softplus(raw) : raw, u = delta * xv;
+    float v = 0.f;
 #pragma unroll
-        for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        v = fmaf(skip, xv, v);
-        if (z) v *= silu(to_float(rz[r]));
-        if (slot[r] < 0) continue;
-        const int n = n0 + r;
-        if (sub == 0) (y + (int64_t)n * p.ld_y)[ch] = from_float<T>(v);
-        float* to = state_out + ((size_t)slot[r] * p.D + ch) * p.S + s0;
-        if (QUADS) {
-            if (s0 < p.S) *reinterpret_cast<float4*>(to) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
-        } else
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (s0 + i < p.S) to[i] = h[r][i];
+    for (int i = 0; i < 8; ++i) {
+        h[i] = fmaf(exp2_approx(delta * a2[i]), fresh ? 0.f : h[i], u * bv[i]);
+        v = s0 + i < p.S ? fmaf(cv[i], h[i], v) : v;
     }
+#pragma unroll
+    for (int o = 1; o < LS; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    v = fmaf(skip, xv, v);
+    if (z) v *= silu(zv);
+    if (slot < 0) return;
+    if (sub == 0) (y + (int64_t)n * p.ld_y)[ch] = from_float<T>(v);
+    float* to = state_out + ((size_t)slot * p.D + ch) * p.S + s0;
+    if (WHOLE) {
+        if (some) store_eight(to, h);
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (s0 + i < p.S) to[i] = h[i];
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------------------
@@ -857,26 +846,22 @@ hts_status forward(ScanArgs p, const hts_scan_inputs& in, T* y, float* state_out
 template <typename T>
 hts_status step(const ScanArgs& p, const hts_scan_inputs& in, const int32_t* slots, int pool, T* y, float* state_out, cudaStream_t s)
 {
-    const bool quads = p.S % 4 == 0 && aligned_to(in.state_in, 16) && aligned_to(state_out, 16) && aligned_to(in.a, 16) && aligned_to(in.b, 4 * sizeof(T)) &&
-                       aligned_to(in.c, 4 * sizeof(T)) && p.ld_b % 4 == 0 && p.ld_c % 4 == 0;
+    bool whole = p.S % 8 == 0 && aligned_to(in.state_in, 32) && aligned_to(state_out, 32) && aligned_to(in.a, 32) && p.ld_b % 8 == 0 && p.ld_c % 8 == 0;
+    for (const void* q : {in.b, in.c}) whole = whole && aligned_to(q, 8 * sizeof(T));
     const T *x = (const T*)in.x, *dt = (const T*)in.dt, *b = (const T*)in.b, *c = (const T*)in.c, *z = (const T*)in.z;
     auto go = [&](auto ls) {
-        constexpr int LS = decltype(ls)::value, ROWS = 2;
-        // two rows a thread where that leaves eight blocks on every SM: 1024 rows of 1024 channels 37 us, with one 40, with four 46
-        const bool many = (int64_t)p.N * p.D * LS / ROWS >= (int64_t)kCoreSms * 1024;
-        const int64_t blocks = (int64_t)(many ? (p.N + ROWS - 1) / ROWS : p.N) * ceil_div((int64_t)p.D * LS, 128);
+        constexpr int LS = decltype(ls)::value;
+        const int64_t blocks = p.N * ceil_div((int64_t)p.D * LS, 128);
         if (blocks > INT32_MAX || (int64_t)p.D * LS > INT32_MAX - 128) return HTS_ERR_INVALID_ARG;
-        auto kernel = many ? (quads ? scan_step_kernel<T, LS, true, ROWS> : scan_step_kernel<T, LS, false, ROWS>)
-                           : (quads ? scan_step_kernel<T, LS, true, 1> : scan_step_kernel<T, LS, false, 1>);
+        auto kernel = whole ? scan_step_kernel<T, LS, true> : scan_step_kernel<T, LS, false>;
         HTS_CUDA(launch_pdl(kernel, dim3((unsigned)blocks), dim3(128), 0, s, p, x, dt, b, c, z, slots, pool, in.state_in, y, state_out));
         note_launch();
         return HTS_OK;
     };
-    if (p.S <= 4) return go(std::integral_constant<int, 1>());
-    if (p.S <= 8) return go(std::integral_constant<int, 2>());
-    if (p.S <= 16) return go(std::integral_constant<int, 4>());
-    if (p.S <= 32) return go(std::integral_constant<int, 8>());
-    return go(std::integral_constant<int, 16>());
+    if (p.S <= 8) return go(std::integral_constant<int, 1>());
+    if (p.S <= 16) return go(std::integral_constant<int, 2>());
+    if (p.S <= 32) return go(std::integral_constant<int, 4>());
+    return go(std::integral_constant<int, 8>());
 }
 
 template <typename T>
