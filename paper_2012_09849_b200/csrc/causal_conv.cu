@@ -210,12 +210,12 @@ __global__ void __launch_bounds__(32 * kWarps, 3) conv_kernel(const ConvArgs p, 
         auto output = [&](auto tap) {
             float r[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float a = b[i];
+            for (int i = 0; i < V; ++i) r[i] = b[i];
 #pragma unroll
-                for (int k = 0; k < W; ++k) a = fmaf(w[k][i], tap(k, i), a);
-                r[i] = p.silu ? silu(a) : a;
-            }
+            for (int k = 0; k < W; ++k) fma_vec<V>(r, w[k], [&](int i) { return tap(k, i); });
+            if (p.silu)
+#pragma unroll
+                for (int i = 0; i < V; ++i) r[i] = silu(r[i]);
             if (q.on) store_vec<V>(to, r);
             to += step_y;
         };
@@ -312,21 +312,19 @@ __global__ void __launch_bounds__(32 * kWarps, 3) conv_gradient_kernel(const Con
                 store_vec<V>(dwindow_in + ((size_t)n * (W - 1) + u + W - 1) * p.D + q.c, g);
         };
         auto slope = [&](auto tap, const float (&raw)[V], float (&g)[V]) {
+            float a[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float a = b[i];
+            for (int i = 0; i < V; ++i) a[i] = b[i];
 #pragma unroll
-                for (int k = 0; k < W; ++k) a = fmaf(w[k][i], tap(k, i), a);
-                g[i] = raw[i] * (p.silu ? silu_slope(a) : 1.f);
-            }
+            for (int k = 0; k < W; ++k) fma_vec<V>(a, w[k], [&](int i) { return tap(k, i); });
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] = raw[i] * (p.silu ? silu_slope(a[i]) : 1.f);
         };
         auto add = [&](auto tap, const float (&g)[V]) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                db[i] += g[i];
+            for (int i = 0; i < V; ++i) db[i] += g[i];
 #pragma unroll
-                for (int k = 0; k < W; ++k) dw[k][i] = fmaf(g[i], tap(k, i), dw[k][i]);
-            }
+            for (int k = 0; k < W; ++k) fma_vec<V>(dw[k], g, [&](int i) { return tap(k, i); });
         };
         for (int t = t0; t < stop; t += G) {
             float in[2][G][V], v[G + W - 1][V], g[G + W - 1][V];
@@ -347,11 +345,9 @@ __global__ void __launch_bounds__(32 * kWarps, 3) conv_gradient_kernel(const Con
                     add(tap, g[W - 1 + j]);
                     float r[V];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        r[i] = 0.f;
+                    for (int i = 0; i < V; ++i) r[i] = 0.f;
 #pragma unroll
-                        for (int k = 0; k < W; ++k) r[i] = fmaf(w[W - 1 - k][i], g[j + k][i], r[i]);
-                    }
+                    for (int k = 0; k < W; ++k) fma_vec<V>(r, w[W - 1 - k], [&](int i) { return g[j + k][i]; });
                     leave(t + j - (W - 1), r);
                 }
 #pragma unroll

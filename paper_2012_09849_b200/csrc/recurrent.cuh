@@ -78,6 +78,19 @@ constexpr float kLog2e = 1.4426950408889634f;
 // 1 / (1 + exp(-v)): 0 and 1 at the infinities
 __device__ __forceinline__ float sigmoid(float v) { return rcp_approx(1.f + exp2_approx(-kLog2e * v)); }
 __device__ __forceinline__ float silu(float v) { return v * sigmoid(v); }
+// a += m b for V neighbours, two a time where there are two; b comes from a function of the neighbour
+template <int V, typename F>
+__device__ __forceinline__ void fma_vec(float (&a)[V], const float (&m)[V], F b)
+{
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 2)
+            asm("{\n\t.reg .b64 ra, rm, rb;\n\tmov.b64 ra, {%0, %1};\n\tmov.b64 rm, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+                "fma.rn.f32x2 ra, rm, rb, ra;\n\tmov.b64 {%0, %1}, ra;\n\t}" : "+f"(a[i]), "+f"(a[i + 1]) : "f"(m[i]), "f"(m[i + 1]), "f"(b(i)), "f"(b(i + 1)));
+    } else
+#pragma unroll
+        for (int i = 0; i < V; ++i) a[i] = fmaf(m[i], b(i), a[i]);
+}
 __device__ __forceinline__ float silu_slope(float v)
 {
     const float q = sigmoid(v);
