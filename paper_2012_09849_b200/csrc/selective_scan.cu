@@ -279,37 +279,40 @@ __global__ void __launch_bounds__(kThreads, 5) scan_kernel(const ScanArgs p, con
     }
 }
 
-// Composes the runs' maps: ends become the runs' first states, `back` what reaches a run from the ones behind it.
-__global__ void __launch_bounds__(256) compose_kernel(const ScanArgs p, const float* state_in, const float* dstate_out, RunMaps m)
+// Composes the runs' maps: ends become the runs' first states, `back` what reaches a run from the ones behind it.  A block has one
+// sequence; sixteen maps are asked for at once, none of them behind another's answer.
+__global__ void __launch_bounds__(128) compose_kernel(const ScanArgs p, const float* state_in, const float* dstate_out, RunMaps m)
 {
     pdl_wait();
     pdl_trigger();
-    const int64_t per = (int64_t)p.D * p.S, id = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)p.N * per;
-    if (id >= all) return;
-    const int n = (int)(id / per);
-    const int64_t chan = id / p.S;                          // n * D + channel
-    const float a2 = p.a[id % per] * kLog2e;
-    float* v = blockIdx.y ? m.back : m.ends;
-    float carry = blockIdx.y ? (dstate_out ? dstate_out[id] : 0.f) : (state_in ? state_in[id] : 0.f);
-    constexpr int G = 8;                                    // loads under way at once
+    const unsigned per = (unsigned)p.D * p.S, across = (per + 127) / 128;       // below 2^31: N D < 2^28 and S <= 64 (too_many)
+    const unsigned at = blockIdx.x % across * 128 + threadIdx.x, n = blockIdx.x / across;
+    if (at >= per) return;
+    const bool back = blockIdx.y;
+    const int64_t all = (int64_t)p.N * per, id = (int64_t)n * per + at, chans = (int64_t)p.N * p.D;
+    const float a2 = p.a[at] * kLog2e;
+    const int r0 = back ? p.runs - 1 : 0, to = back ? -1 : 1;
+    float *v = (back ? m.back : m.ends) + id + r0 * all;
+    const float* sums = m.sums + (int64_t)n * p.D + at / p.S + r0 * chans;
+    const uint8_t* broken = m.broken + n + (int64_t)r0 * p.N;
+    float carry = back ? (dstate_out ? dstate_out[id] : 0.f) : (state_in ? state_in[id] : 0.f);
+    constexpr int G = 16;
     for (int i0 = 0; i0 < p.runs; i0 += G) {
-        float e[G] = {}, keep[G] = {};
+        float e[G], sum[G];
+        uint8_t cut[G];
 #pragma unroll
-        for (int k = 0; k < G; ++k) {
-            const int r = blockIdx.y ? p.runs - 1 - (i0 + k) : i0 + k;
-            if (r >= 0 && r < p.runs - (blockIdx.y ? 0 : 1)) {           // the last run's end is not asked for
-                e[k] = v[(int64_t)r * all + id];
-                keep[k] = m.broken[(int64_t)r * p.N + n] ? -1.f : exp2_approx(a2 * m.sums[(int64_t)r * p.N * p.D + chan]);
+        for (int k = 0; k < G; ++k)
+            if (i0 + k < p.runs - 1) {                                          // the last map of all leads nowhere
+                e[k] = v[to * (i0 + k) * all];
+                sum[k] = sums[to * (i0 + k) * chans];
+                cut[k] = broken[(int64_t)to * (i0 + k) * p.N];
             }
-        }
 #pragma unroll
-        for (int k = 0; k < G; ++k) {
-            const int r = blockIdx.y ? p.runs - 1 - (i0 + k) : i0 + k;
-            if (r >= 0 && r < p.runs) {
-                v[(int64_t)r * all + id] = carry;
-                carry = keep[k] < 0.f ? e[k] : fmaf(keep[k], carry, e[k]);
+        for (int k = 0; k < G; ++k)
+            if (i0 + k < p.runs) {
+                v[to * (i0 + k) * all] = carry;
+                if (i0 + k < p.runs - 1) carry = cut[k] ? e[k] : fmaf(exp2_approx(a2 * sum[k]), carry, e[k]);
             }
-        }
     }
 }
 
@@ -767,7 +770,7 @@ Plan plan(int T, int N, int D, int S, bool gradient)
     Plan q{};
     const int ls = gradient_lanes(S);
     q.across = gradient ? ceil_div(D, 2 * kThreads / ls) : channel_blocks(D, scan_shape(S));
-    cut_runs(T, q.across * N, (int64_t)kCoreSms * (gradient ? 4 : 6), gradient ? 4 * kChunk : 4 * kGroup, &q.runs, &q.length);
+    cut_runs(T, q.across * N, (int64_t)kCoreSms * (gradient ? 6 : 8), gradient ? 4 * kChunk : 4 * kGroup, &q.runs, &q.length);
     size_t at = 0;
     auto take = [&](size_t floats) { const size_t was = at; at += round256(floats * 4); return was; };
     const size_t states = (size_t)N * D * S;
@@ -801,8 +804,8 @@ ScanArgs scan_args(const hts_scan_desc& d, const hts_scan_inputs& in)
 }
 hts_status launch_compose(const ScanArgs& p, const float* state_in, const float* dstate_out, const RunMaps& m, bool back, cudaStream_t s)
 {
-    const int64_t blocks = ceil_div((int64_t)p.N * p.D * p.S, 256);
-    HTS_CUDA(launch_pdl(compose_kernel, dim3((unsigned)blocks, back ? 2 : 1), dim3(256), 0, s, p, state_in, dstate_out, m));
+    const int64_t blocks = p.N * ceil_div((int64_t)p.D * p.S, 128);
+    HTS_CUDA(launch_pdl(compose_kernel, dim3((unsigned)blocks, back ? 2 : 1), dim3(128), 0, s, p, state_in, dstate_out, m));
     note_launch();
     return HTS_OK;
 }
@@ -923,7 +926,7 @@ bool far(int64_t N, std::initializer_list<int64_t> strides)
 // Blocks of one launch, of every kind: a grid has fewer than 2^31.
 bool too_many(int64_t T, int64_t N, int64_t D)
 {
-    return T * N > ((int64_t)1 << 31) || N * D >= kMostInStep || N >= kMostInStep / 128 || ceil_div(D, 16) * N * ceil_div(T, 32) > INT32_MAX;
+    return T * N > ((int64_t)1 << 31) || N * D >= kMostInStep || D >= 1 << 24 || N >= kMostInStep / 128 || ceil_div(D, 16) * N * ceil_div(T, 32) > INT32_MAX;
 }
 bool bad(const hts_scan_desc* d, const hts_scan_inputs* in, bool with_steps)
 {
