@@ -391,7 +391,9 @@ hts_status hts_policy_step_noalloc(const hts_net_desc *desc, const hts_weights *
  * Workspaces are the caller's: DEVICE memory on a 16-byte boundary, at least as many bytes as the
  * function of the same name and `_workspace` returns (0 for sizes that the call refuses), not used by anything else
  * until the call's work is done; its contents need not be kept.  Calls with workspaces of their own
- * are independent, also across streams, threads and captured graphs.  Nothing is allocated.       */
+ * are independent, also across streams, threads and captured graphs.  Nothing is allocated.
+ * Sizes: T, rows and features up to 2^30; the scan further has T*N up to 2^30, and N times every ld below 2^28.  Larger
+ * ones are refused with HTS_ERR_INVALID_ARG.                                             */
 #define HTS_ACT_NONE 0
 #define HTS_ACT_RELU 1
 #define HTS_ACT_SILU 2 /* v / (1 + exp(-v))          */
@@ -502,7 +504,8 @@ hts_status hts_linear(const hts_linear_desc *desc, const void *x, const void *w,
 /* Its gradients, given dy:  dz = dy act'(pre), dx = dz w, dw = dz^T x, dbias = sum of dz; the residual's is dy.
  *   pre rows bf16, as hts_linear left them (not read for HTS_ACT_NONE);  dx rows bf16;  dw [out_features,in_features];
  *   dbias f32: each may be NULL, not all.
- * With an activation dz is rounded to bf16 for the products (dbias adds it unrounded); sums in fp32, in a fixed order.  */
+ * With an activation dz is rounded to bf16 for the products (for rows * out_features up to 2^18 to two bf16 numbers that
+ * add up to it; dbias adds it unrounded); sums in fp32, in a fixed order.               */
 hts_status hts_linear_gradient(const hts_linear_desc *desc, const void *x, const void *w, const void *pre_or_null,
                                const void *dy, void *dx, void *dw, float *dbias, void *workspace, int64_t workspace_bytes,
                                void *cuda_stream);

@@ -549,9 +549,10 @@ hts_status gradient(ConvArgs p, int width, const T* x, const T* win, const T* dy
     return launch_column_sums({part, rows, cols, (int64_t)width * p.D, p.D, width, dw, db, cols, nullptr}, s);
 }
 
+constexpr int kMostSteps = 1 << 30;             // a run's end is counted in 32 bits
 bool bad(const hts_conv_desc* d, bool with_steps)
 {
-    return !d || (with_steps && d->T < 1) || d->N < 1 || d->channels < 1 || d->width < 2 || d->width > 4 || d->ld_x < d->channels ||
+    return !d || (with_steps && (d->T < 1 || d->T > kMostSteps)) || d->N < 1 || d->channels < 1 || d->width < 2 || d->width > 4 || d->ld_x < d->channels ||
            (d->dtype != HTS_DTYPE_FP32 && d->dtype != HTS_DTYPE_BF16) || (d->activation != HTS_ACT_NONE && d->activation != HTS_ACT_SILU);
 }
 
@@ -570,7 +571,7 @@ using namespace hts;
 
 extern "C" int64_t hts_causal_conv_workspace(int32_t T, int32_t N, int32_t channels, int32_t width)
 {
-    if (T < 1 || N < 1 || channels < 1 || width < 2 || width > 4) return 0;
+    if (T < 1 || T > kMostSteps || N < 1 || channels < 1 || width < 2 || width > 4) return 0;
     int64_t rows = 0;
     for (int V : {1, kGradVector}) {                // whichever form the pointers' alignment allows
         if (channels % V) continue;

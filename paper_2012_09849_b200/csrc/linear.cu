@@ -767,9 +767,10 @@ LinearPlan linear_plan(int M, int K, int N, bool gradient)
     q.bytes = at;
     return q;
 }
+constexpr int kMostRows = 1 << 30;              // tiles' corners are counted in 32 bits
 bool bad(const hts_linear_desc* d)
 {
-    return !d || d->rows < 1 || d->in_features < 1 || d->out_features < 1 || d->activation < HTS_ACT_NONE || d->activation > HTS_ACT_GELU ||
+    return !d || d->rows < 1 || d->in_features < 1 || d->out_features < 1 || d->rows > kMostRows || d->in_features > kMostRows || d->out_features > kMostRows || d->activation < HTS_ACT_NONE || d->activation > HTS_ACT_GELU ||
            d->ld_x < d->in_features || ceil_div(d->rows, 128) * ceil_div(d->out_features, 64) > INT32_MAX / 8 ||
            ceil_div(d->rows, 128) * ceil_div(d->in_features, 64) > INT32_MAX / 8 || (int64_t)d->out_features * d->in_features > ((int64_t)1 << 38);
 }
@@ -781,7 +782,7 @@ using namespace hts;
 
 extern "C" int64_t hts_linear_workspace(int32_t rows, int32_t in_features, int32_t out_features, int32_t gradient)
 {
-    if (rows < 1 || in_features < 1 || out_features < 1) return 0;
+    if (rows < 1 || in_features < 1 || out_features < 1 || rows > kMostRows || in_features > kMostRows || out_features > kMostRows) return 0;
     return (int64_t)linear_plan(rows, in_features, out_features, gradient != 0).bytes;
 }
 

@@ -926,7 +926,7 @@ bool far(int64_t N, std::initializer_list<int64_t> strides)
 // Blocks of one launch, of every kind: a grid has fewer than 2^31.
 bool too_many(int64_t T, int64_t N, int64_t D)
 {
-    return T * N > ((int64_t)1 << 31) || N * D >= kMostInStep || D >= 1 << 24 || N >= kMostInStep / 128 || ceil_div(D, 16) * N * ceil_div(T, 32) > INT32_MAX;
+    return T * N > ((int64_t)1 << 30) || N * D >= kMostInStep || D >= 1 << 24 || N >= kMostInStep / 128 || ceil_div(D, 16) * N * ceil_div(T, 32) > INT32_MAX;
 }
 bool bad(const hts_scan_desc* d, const hts_scan_inputs* in, bool with_steps)
 {
