@@ -61,10 +61,20 @@ __device__ __forceinline__ Quad load_quad(const float* at)
 // (a third of a last place; measured over each part of that range), and a decay near 1 acts for hundreds of steps, so that the
 // sums drift: states of a 128-step rollout off by 2.1e-6.  Adding 2.3e-8 to the exponent, in the multiply-add that forms it, takes
 // the mean out (it is within 5e-9): 0.5e-6.
+constexpr float kMeanError = 2.3e-8f;
 __device__ __forceinline__ f32x2 decay_pair(f32x2 delta, f32x2 a2)
 {
-    const f32x2 v = fma2(delta, a2, both(2.3e-8f));
+    const f32x2 v = fma2(delta, a2, both(kMeanError));
     return pair(exp2_approx(lane_of(v, 0)), exp2_approx(lane_of(v, 1)));
+}
+
+// Finite, unless it is NaN: the product of a run's decays, which may grow beyond all bounds where nothing is handed back.
+__device__ __forceinline__ f32x2 held(f32x2 v)
+{
+    float lo = lane_of(v, 0), hi = lane_of(v, 1);
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(lo) : "f"(3e38f));
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(hi) : "f"(3e38f));
+    return pair(lo, hi);
 }
 
 // log(1 + exp(v)) = max(v, 0) + log(1 + e), e = exp(-|v|); log(1 + e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by atanh's power
@@ -250,7 +260,7 @@ __global__ void __launch_bounds__(kThreads, 5) scan_kernel(const ScanArgs p, con
                         h[i + k] = fma2(decay, h[i + k], mul2(u2, bb[k]));
                         if (MODE == SCAN) acc[k] = fma2(cc[k], h[i + k], acc[k]);
                         if (MODE == MAPS_BACK && !broken) {
-                            prod[i + k] = mul2(prod[i + k], decay);
+                            prod[i + k] = held(mul2(prod[i + k], decay));
                             back[i + k] = fma2(mul2(both(gate), cc[k]), prod[i + k], back[i + k]);
                         }
                     }
@@ -311,7 +321,7 @@ __global__ void __launch_bounds__(128) compose_kernel(const ScanArgs p, const fl
         for (int k = 0; k < G; ++k)
             if (i0 + k < p.runs) {
                 v[to * (i0 + k) * all] = carry;
-                if (i0 + k < p.runs - 1) carry = cut[k] ? e[k] : fmaf(exp2_approx(a2 * sum[k]), carry, e[k]);
+                if (i0 + k < p.runs - 1) carry = cut[k] || carry == 0.f ? e[k] : fmaf(exp2_approx(a2 * sum[k]), carry, e[k]);      // a zero stays one under any growth
             }
     }
 }
@@ -330,7 +340,7 @@ __device__ __forceinline__ void store_eight(float* p, const float (&v)[8])
                  ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
 }
 // One step of row n over the states at its slot: eight states a thread, LS lanes a channel.  A row whose slot lies outside the pool is
-// left alone.  Bound by the states, which are read and written once: 1024 rows of 1024 channels and 16 states in 29.6 us, 4.8 TB/s.  With
+// left alone.  Bound by the states, which are read and written once: 1024 rows of 1024 channels and 16 states in 29.2 us, 4.9 TB/s.  With
 // four states a thread, four lanes computed each channel's delta and gate (37 us); two or four rows a thread take as long as one.
 // WHOLE: eight states are one access of 32 bytes.
 template <typename T, int LS, bool WHOLE>
@@ -369,7 +379,7 @@ __global__ void __launch_bounds__(128) scan_step_kernel(const ScanArgs p, const 
     float v = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        h[i] = fmaf(exp2_approx(delta * a2[i]), fresh ? 0.f : h[i], u * bv[i]);
+        h[i] = fmaf(exp2_approx(fmaf(delta, a2[i], kMeanError)), fresh ? 0.f : h[i], u * bv[i]);
         v = s0 + i < p.S ? fmaf(cv[i], h[i], v) : v;
     }
 #pragma unroll
@@ -417,7 +427,7 @@ template <typename T, int LS> struct GradientShared {
 // channel) crosses LS lanes, what has to be added over channels (dB and dC, eight sums, two channels of which meet in the thread)
 // the others: in the first exchanges of each each lane keeps half of the sums and hands on the other half.  With eight states of one
 // channel in a thread, states and gradients in shared memory and the sums over channels read from there, shared memory
-// bounded it (105 accesses a warp and step): 1165 us for 128 x 256 steps of 1024 channels and 16 states, as long as this takes (1135),
+// bounded it (105 accesses a warp and step): 1165 us for 128 x 256 steps of 1024 channels and 16 states, as long as this takes (1132),
 // which has 42 % of the accesses and is bound by latency: three warps a scheduler of 160 registers, 0.53 instructions a clock.  Four
 // with states of two steps (1201) or chunks of four (1077, but twice the memory for checks) do not change that much.
 template <typename T, int LS, bool WIDE>

@@ -294,3 +294,51 @@ def test_advantages_are_a_scan():
     hts.hts_selective_scan(flip(delta), one, torch.full((1, 1), float(torch.log(torch.tensor(gamma * lam))), device="cuda"), one, one, None, None, None,
                            done.flip(0).contiguous(), None, None, False, y, None, torch.empty(hts.hts_selective_scan_workspace(T, N, 1, 1), dtype=torch.uint8, device="cuda"))
     assert float((y[..., 0].flip(0) - adv).abs().max()) <= slack(T) * float(adv.abs().max()) * 20      # 1 / (1 - gamma lambda) steps matter
+
+
+def test_growth_of_nothing_is_nothing():
+    """Decays above 1 whose product over a run of steps is beyond fp32, where there is nothing to multiply: before the first input, behind the last output."""
+    T, D, S = 100, 8, 13
+    c = case(T, 1, D, S, softplus=False, p=0.0, state=False)
+    c["dt"] = torch.full_like(c["dt"], 8.0)
+    c["a"] = torch.full_like(c["a"], 0.5)                       # e^4 a step
+    c["x"] = c["x"].clone()
+    c["x"][:-8] = 0
+    y, out = run(c)
+    (ry, rh), (my, mh) = ref.scan(**wide(c)), magnitudes(c)
+    ref.within(y, ry, slack(T) * my)
+    ref.within(out, rh, slack(T) * mh)
+    dy = torch.randn_like(y)
+    dy[8:] = 0
+    got, want = gradient(c, dy, None), reference_gradient(c, dy, None)
+    for k in got:                                               # an exponent of 4 log2(e) is rounded by less than 2^-21 a step
+        if k != "state_in":
+            assert bool(torch.isfinite(got[k]).all()) and ref.rel2(got[k], want[k]) <= 2 * slack(T), k
+
+
+def test_steps_of_no_length_keep_the_state():
+    c = case(40, 3, 24, 13, p=0.0, softplus=False)
+    c["dt"] = torch.zeros_like(c["dt"])
+    y, out = run(c)
+    assert torch.equal(out, c["state_in"])
+    for S in (13, 16):
+        c = case(1, 3, 24, S, p=0.0, softplus=False)
+        states = torch.empty_like(c["state_in"])
+        hts.hts_selective_scan_step(c["x"][0], torch.zeros_like(c["dt"][0]), c["a"], c["b"][0], c["c"][0], None, None, None, None, None, c["state_in"], False, torch.empty_like(c["x"][0]),
+                                    states)
+        assert torch.equal(states, c["state_in"])
+
+
+def test_many_single_steps_do_not_drift():
+    """Decays near one over 2000 steps: what a decay is off by on average adds up over the steps that a state lives, 1 / (1 - decay) of them."""
+    T, D, S = 2000, 16, 16
+    c = case(T, 1, D, S, p=0.0, softplus=False, gate=False, skip=False)
+    c["a"] = -(0.5 + torch.rand_like(c["a"]))
+    c["dt"] = torch.full_like(c["dt"], 1e-3)
+    c["x"], c["b"] = c["x"].abs() + 1, c["b"].abs() + 1         # nothing cancels
+    state, y = c["state_in"].abs(), torch.empty(1, D, device="cuda")
+    c["state_in"] = state.clone()
+    for t in range(T):
+        hts.hts_selective_scan_step(c["x"][t], c["dt"][t], c["a"], c["b"][t], c["c"][t], None, None, None, None, None, state, False, y, state)
+    _, want = ref.scan(**wide(c))
+    assert ref.rel2(state, want) <= 700 * 2.0 ** -24            # a life of 2000 steps at most, each off by 1e-8 on average and at random by a rounding
