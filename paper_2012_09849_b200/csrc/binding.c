@@ -169,8 +169,8 @@ static int look(PyObject *x, const char *name, int want, Seen *v)
     return int_ptr(PyObject_CallMethodNoArgs(x, s_data_ptr), &v->ptr);
 }
 /* memory of the CUDA device that was current when the call began (began()); what is not is reported when all else is right */
-static long g_current;
-static const char *g_elsewhere, *g_where;
+static __thread long g_current;                      /* of this thread's call: a tensor's attributes may run Python, which lets other threads in */
+static __thread const char *g_elsewhere, *g_where;
 static int began(void)
 {
     if (!torch_types()) return 0;

@@ -499,7 +499,6 @@ hts_status forward(ConvArgs p, int width, const T* x, const T* win, T* y, T* wou
     const bool wide = vectors(p.D, kVector * sizeof(T), {x, win, y, wout}, {p.ld_x, p.ld_y});
     cut_runs(p, wide ? kVector : 1, kGroup);
     const int64_t blocks = run_blocks(p) * ceil_div(p.lanes, 32);
-    if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
     return by_width(width, [&](auto k) {
         constexpr int W = decltype(k)::value;
         static OncePerDevice allowed[2];
@@ -532,7 +531,6 @@ hts_status gradient(ConvArgs p, int width, const T* x, const T* win, const T* dy
                       aligned_to(dwin, kGradVector * sizeof(float));
     cut_runs(p, wide ? kGradVector : 1, kGradientRun);
     const int64_t rows = run_blocks(p), blocks = rows * ceil_div(p.lanes, 32);
-    if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
     const bool sums = dw || db;
     const hts_status st = by_width(width, [&](auto k) {
         constexpr int W = decltype(k)::value;
@@ -549,10 +547,15 @@ hts_status gradient(ConvArgs p, int width, const T* x, const T* win, const T* dy
     return launch_column_sums({part, rows, cols, (int64_t)width * p.D, p.D, width, dw, db, cols, nullptr}, s);
 }
 
-constexpr int kMostSteps = 1 << 30;             // a run's end is counted in 32 bits
+constexpr int kMost = 1 << 30;                  // a run's end is counted in 32 bits
+// T = 1 for single steps
+bool bad_sizes(int64_t T, int64_t N, int64_t D, int width)
+{
+    return T < 1 || N < 1 || D < 1 || T > kMost || N > kMost || D > kMost || N * D > ((int64_t)1 << 38) || width < 2 || width > 4;      // blocks of channels and runs: below 2^31
+}
 bool bad(const hts_conv_desc* d, bool with_steps)
 {
-    return !d || (with_steps && (d->T < 1 || d->T > kMostSteps)) || d->N < 1 || d->channels < 1 || d->width < 2 || d->width > 4 || d->ld_x < d->channels ||
+    return !d || bad_sizes(with_steps ? d->T : 1, d->N, d->channels, d->width) || d->ld_x < d->channels ||
            (d->dtype != HTS_DTYPE_FP32 && d->dtype != HTS_DTYPE_BF16) || (d->activation != HTS_ACT_NONE && d->activation != HTS_ACT_SILU);
 }
 
@@ -571,7 +574,7 @@ using namespace hts;
 
 extern "C" int64_t hts_causal_conv_workspace(int32_t T, int32_t N, int32_t channels, int32_t width)
 {
-    if (T < 1 || T > kMostSteps || N < 1 || channels < 1 || width < 2 || width > 4) return 0;
+    if (bad_sizes(T, N, channels, width)) return 0;
     int64_t rows = 0;
     for (int V : {1, kGradVector}) {                // whichever form the pointers' alignment allows
         if (channels % V) continue;

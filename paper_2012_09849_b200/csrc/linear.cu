@@ -10,7 +10,7 @@
 // Large products run on pairs of SMs, 256 x 256 outputs a pair, persistent, with two accumulators in tensor memory so that one
 // tile's epilogue runs under the next one's products.  A pair of SMs needs 64 bytes of operands from L2 per SM and tensor clock,
 // a 128 x 256 tile on a single SM 96, and L2 delivers about 50.  Few tiles (a step of few rows) are cut along k over
-// clusters of up to eight SMs: each forms a partial 128 x 64 tile, leaves it in its shared memory, and the cluster adds them in rank
+// clusters of up to eight SMs: each forms a partial tile (128 x 64 or 128 x 128), leaves it in its shared memory, and the cluster adds them in rank
 // order and runs the epilogue, in the same launch.  dw has few tiles and a long k: pairs take ranges of k and leave planes
 // of fp32 sums, which a second kernel adds in order.
 //
@@ -74,16 +74,17 @@ __device__ __forceinline__ float activate(float v, int act)
     if (act == HTS_ACT_GELU) return v * normal_cdf(v, bell);
     return v;
 }
-__device__ __forceinline__ float slope_of(float v, int act)
+// dy act'(v); nothing passes where ReLU is shut, infinite or not
+__device__ __forceinline__ float through(float dy, float v, int act)
 {
-    float bell;
-    if (act == HTS_ACT_RELU) return v > 0.f ? 1.f : 0.f;
-    if (act == HTS_ACT_SILU) return silu_slope(v);
-    if (act == HTS_ACT_GELU) {
+    float bell, slope;
+    if (act == HTS_ACT_RELU) return v <= 0.f ? 0.f : dy;
+    if (act == HTS_ACT_SILU) slope = silu_slope(v);
+    else {
         const float c = normal_cdf(v, bell);
-        return fmaf(v * 0.39894228f, bell, c);
+        slope = fmaf(v * 0.39894228f, bell, c);
     }
-    return 1.f;
+    return __fmul_rn(dy, slope);            // the same whether dz is stored or only added
 }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 {
@@ -596,7 +597,7 @@ __global__ void __launch_bounds__(256) dz_kernel(const bf16* dy, int64_t ld_dy, 
             if (pre) {
                 const Vec<bf16, V> u = load_vec<V>(pre + row * ld_pre + c);
 #pragma unroll
-                for (int k = 0; k < V; ++k) v[k] = __fmul_rn(v[k], slope_of(to_float(u.v[k]), act));     // the same whether dz is stored or only added
+                for (int k = 0; k < V; ++k) v[k] = through(v[k], to_float(u.v[k]), act);
             }
 #pragma unroll
             for (int k = 0; k < V; ++k) sum[k] += v[k];
@@ -768,11 +769,15 @@ LinearPlan linear_plan(int M, int K, int N, bool gradient)
     return q;
 }
 constexpr int kMostRows = 1 << 30;              // tiles' corners are counted in 32 bits
+constexpr int64_t kMostElements = (int64_t)1 << 38;
+// Sizes out of range: of one axis, or so many tiles, row blocks or weights that a grid cannot count them.
+bool bad_sizes(int64_t M, int64_t K, int64_t N)
+{
+    return M < 1 || K < 1 || N < 1 || M > kMostRows || K > kMostRows || N > kMostRows || M * K > kMostElements || M * N > kMostElements || N * K > kMostElements;
+}
 bool bad(const hts_linear_desc* d)
 {
-    return !d || d->rows < 1 || d->in_features < 1 || d->out_features < 1 || d->rows > kMostRows || d->in_features > kMostRows || d->out_features > kMostRows || d->activation < HTS_ACT_NONE || d->activation > HTS_ACT_GELU ||
-           d->ld_x < d->in_features || ceil_div(d->rows, 128) * ceil_div(d->out_features, 64) > INT32_MAX / 8 ||
-           ceil_div(d->rows, 128) * ceil_div(d->in_features, 64) > INT32_MAX / 8 || (int64_t)d->out_features * d->in_features > ((int64_t)1 << 38);
+    return !d || bad_sizes(d->rows, d->in_features, d->out_features) || d->activation < HTS_ACT_NONE || d->activation > HTS_ACT_GELU || d->ld_x < d->in_features;
 }
 
 }  // namespace
@@ -782,7 +787,7 @@ using namespace hts;
 
 extern "C" int64_t hts_linear_workspace(int32_t rows, int32_t in_features, int32_t out_features, int32_t gradient)
 {
-    if (rows < 1 || in_features < 1 || out_features < 1 || rows > kMostRows || in_features > kMostRows || out_features > kMostRows) return 0;
+    if (bad_sizes(rows, in_features, out_features)) return 0;
     return (int64_t)linear_plan(rows, in_features, out_features, gradient != 0).bytes;
 }
 
@@ -828,7 +833,6 @@ extern "C" hts_status hts_linear_gradient(const hts_linear_desc* d, const void* 
         float* part = dbias ? (float*)(ws + q.sums) : nullptr;
         const bool wide = N % 8 == 0 && as_is(dy, d->ld_dy) && (!pre || as_is(pre, d->ld_pre));
         const int64_t blocks = ceil_div(M, kSumRows) * ceil_div(N, wide ? 256 : 32);
-        if (blocks > INT32_MAX) return HTS_ERR_INVALID_ARG;
         HTS_CUDA(launch_pdl(wide ? dz_kernel<8> : dz_kernel<1>, dim3((unsigned)blocks), dim3(32, 8), 0, s, (const bf16*)dy, d->ld_dy, (const bf16*)pre, d->ld_pre, M, N,
                             d->activation, dz, padded(N), act && dz_planes(M, N) > 1, part));
         note_launch();

@@ -183,3 +183,20 @@ def test_two_calls_at_once():
         got = [run(c, "silu", stream=s)[0] for c, s in zip(cases, streams)]
         torch.cuda.synchronize()
         assert all(torch.equal(u, v) for u, v in zip(got, want))
+
+
+@pytest.mark.parametrize("M,N", [(40, 72), (41, 71), (4100, 72)])
+def test_nothing_passes_where_relu_is_shut(M, N):
+    """An infinite or undefined dy in front of a pre-activation of zero or less."""
+    c = case(M, 64, N, residual=False)
+    _, pre = run(c, "relu", keep=True)
+    pre[3, 5], pre[M - 1, 0] = -1.0, 0.0
+    dy = rows(M, N, 0, 9).clone()
+    clean = torch.where(pre > 0, dy, torch.zeros_like(dy))
+    dy[3, 5], dy[M - 1, 0] = float("inf"), float("nan")
+    results = []
+    for d in (dy, clean):
+        dx, dw, db = torch.empty(M, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(N, 64, device="cuda"), torch.empty(N, device="cuda")
+        hts.hts_linear_gradient(c["x"], c["w"], pre, d, "relu", dx, dw, db, torch.empty(hts.hts_linear_workspace(M, 64, N, True), dtype=torch.uint8, device="cuda"))
+        results.append((dx, dw, db))
+    assert all(bool(torch.isfinite(u).all()) and torch.equal(u, v) for u, v in zip(*results))

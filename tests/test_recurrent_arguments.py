@@ -147,3 +147,39 @@ def test_tensors_of_the_others():
         hts.hts_linear_gradient(**grad)
     with pytest.raises(TypeError):                       # not a dict
         hts.hts_selective_scan_gradient(**{k: None if k in ("y", "state_out") else v for k, v in good.items() if k not in ("y", "state_out")}, dy=x, dstate_out=None, grads=[])
+
+
+def test_a_size_that_a_call_refuses_has_no_workspace():
+    big = 1 << 30
+    assert hts.hts_causal_conv_workspace(big + 1, 1, 8, 4) == hts.hts_causal_conv_workspace(4, big, 512, 4) == hts.hts_causal_conv_workspace(4, big + 1, 8, 4) == 0
+    assert hts.hts_linear_workspace(big, 512, 8) == hts.hts_linear_workspace(8, big, 512, True) == hts.hts_linear_workspace(512, 8, big) == 0
+    assert hts.hts_selective_scan_workspace(big, 2, 8, 16) == hts.hts_selective_scan_workspace(4, 1 << 21, 8, 16) == hts.hts_selective_scan_workspace(1 << 20, 16, 1 << 20, 16, True) == 0
+    for sizes in (dict(T=4, N=big, channels=512, ld_x=512, ld_y=512), dict(T=4, N=big + 1), dict(T=big + 1)):
+        assert conv(**sizes) == INVALID
+    for sizes in (dict(rows=big, in_features=512, ld_x=512), dict(rows=512, out_features=big, ld_y=big, ld_pre=big, ld_residual=big)):
+        assert linear_call(**sizes, bytes=1 << 60) == INVALID
+    for sizes in (dict(T=big, N=2), dict(N=1 << 21)):
+        assert scan_call(**sizes, bytes=1 << 60) == INVALID
+
+
+def test_threads_do_not_see_each_others_tensors():
+    """A tensor whose attributes run Python lets another thread's call in between the checks of this one, which reports its own first fault all the same."""
+    import threading
+    calls = []
+
+    class Slow(torch.Tensor):
+        @classmethod
+        def __torch_function__(cls, func, types, args=(), kwargs=None):
+            if getattr(func, "__name__", "") == "stride":
+                def other():
+                    with pytest.raises(TypeError):
+                        hts.hts_causal_conv(**conv_tensors(x=5))
+                    calls.append(1)
+                t = threading.Thread(target=other)
+                t.start()
+                t.join()
+            return super().__torch_function__(func, types, args, kwargs or {})
+
+    with pytest.raises(ValueError, match="x is not on a CUDA device"):
+        hts.hts_causal_conv(**conv_tensors(window_out=torch.zeros(2, 3, 8).as_subclass(Slow)))
+    assert calls
