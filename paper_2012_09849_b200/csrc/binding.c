@@ -121,80 +121,102 @@ static int to_stream(PyObject *x, void **out)
     return !PyErr_Occurred();
 }
 
-/* ---- tensors of the recurrent core: the library is told sizes and strides, so that they are read off the tensors ---- */
-static PyObject *g_types[4], *s_dtype, *s_shape, *s_stride, *s_get_device, *s_nbytes;      /* torch.float32, bfloat16, uint8, int32 */
+/* ---- tensors of the recurrent core: the library is told sizes and strides, so that they are read off the tensors ----
+ * By DLPack's table of C functions (version 1), which torch.Tensor carries: one call tells all of a tensor, in 30 ns
+ * instead of the 330 of its Python attributes.  A single scan step has fourteen tensors and takes 2 us on the device. */
+typedef struct {
+    void *data;
+    int32_t device_type, device, dims;
+    uint8_t kind, bits;
+    uint16_t lanes;
+    int64_t *size, *stride;                            /* the tensor's own; strides in elements */
+    uint64_t offset;
+} View;
+typedef struct Exchange {
+    uint32_t major, minor;
+    const struct Exchange *older;
+    void *allocate, *take, *give;                      /* of tensors that change hands: not used */
+    int (*view)(void *object, View *out);              /* nothing is kept alive; -1 with an exception set on failure */
+    int (*current_stream)(int32_t device_type, int32_t device, void **out);
+} Exchange;
+enum { ON_CUDA = 2 };                                  /* DLPack's device type */
+static const Exchange *g_exchange;
 static PyTypeObject *g_tensor;
+static PyObject *g_current_device;                     /* torch._C._cuda_getDevice */
 enum { F32_T = 0, BF16_T = 1, U8_T = 2, I32_T = 3 };                                 /* the first two are HTS_DTYPE_* */
 
-static int torch_types(void)
+static int torch_tensors(void)
 {
-    static const char *const names[4] = {"float32", "bfloat16", "uint8", "int32"};
     if (g_tensor) return 1;
-    PyObject *torch = PyImport_ImportModule("torch"), *c = torch ? PyObject_GetAttrString(torch, "_C") : NULL;
-    for (int i = 0; c && i < 4; ++i)
-        if (!g_types[i] && !(g_types[i] = PyObject_GetAttrString(torch, names[i]))) Py_CLEAR(c);
-    if (c && !g_get_device) g_get_device = PyObject_GetAttrString(c, "_cuda_getDevice");
-    PyObject *t = c && g_get_device ? PyObject_GetAttrString(torch, "Tensor") : NULL;
-    Py_XDECREF(torch); Py_XDECREF(c);
+    PyObject *torch = PyImport_ImportModule("torch"), *t = torch ? PyObject_GetAttrString(torch, "Tensor") : NULL;
+    PyObject *c = t ? PyObject_GetAttrString(torch, "_C") : NULL, *capsule = c ? PyObject_GetAttrString(t, "__dlpack_c_exchange_api__") : NULL;
+    const Exchange *e = capsule ? PyCapsule_GetPointer(capsule, "dlpack_exchange_api") : NULL;     /* lives as long as the process */
+    while (e && e->major != 1) e = e->older;
+    if (capsule && !e && !PyErr_Occurred()) PyErr_SetString(PyExc_ImportError, "torch has no DLPack functions of version 1");
+    if (e && !g_current_device && !(g_current_device = PyObject_GetAttrString(c, "_cuda_getDevice"))) e = NULL;
+    Py_XDECREF(torch); Py_XDECREF(c); Py_XDECREF(capsule);
+    if (!e) { Py_XDECREF(t); return 0; }
+    g_exchange = e;
     g_tensor = (PyTypeObject *)t;
-    return t != NULL;
+    return 1;
 }
 static int refuse(PyObject *type, const char *name, const char *why)
 {
     PyErr_Format(type, "%s %s", name, why);
     return 0;
 }
-static int int64_at(PyObject *tuple, Py_ssize_t i, int64_t *out)
-{
-    *out = PyLong_AsLongLong(PyTuple_GET_ITEM(tuple, i));
-    return !(*out == -1 && PyErr_Occurred());
-}
 /* A tensor: its type, sizes and strides (at most four).  want < 0: of fp32 or bf16. */
-typedef struct { int type, dims; int64_t size[4], stride[4]; void *ptr; } Seen;
-static int look(PyObject *x, const char *name, int want, Seen *v)
+typedef struct { int type, dims; int64_t size[4], stride[4]; void *ptr; int device; } Seen;
+static int view(PyObject *x, const char *name, View *v)
 {
-    if (!torch_types()) return 0;
     if (!PyObject_TypeCheck(x, g_tensor)) return refuse(PyExc_TypeError, name, "is not a tensor");
-    PyObject *t = PyObject_GetAttr(x, s_dtype);
-    if (!t) return 0;
-    for (v->type = 0; v->type < 4 && t != g_types[v->type]; ++v->type) { }
-    Py_DECREF(t);
-    if (want < 0 ? v->type > BF16_T : v->type != want) return refuse(PyExc_TypeError, name, "has the wrong element type");
-    PyObject *sz = PyObject_GetAttr(x, s_shape), *st = sz ? PyObject_CallMethodNoArgs(x, s_stride) : NULL;
-    int ok = st && PyTuple_Check(sz) && PyTuple_Check(st) && PyTuple_GET_SIZE(sz) <= 4;
-    v->dims = ok ? (int)PyTuple_GET_SIZE(sz) : 0;
-    for (int i = 0; ok && i < v->dims; ++i) ok = int64_at(sz, i, &v->size[i]) && int64_at(st, i, &v->stride[i]);
-    Py_XDECREF(sz); Py_XDECREF(st);
-    if (!ok) return PyErr_Occurred() ? 0 : refuse(PyExc_ValueError, name, "has the wrong shape");
-    return int_ptr(PyObject_CallMethodNoArgs(x, s_data_ptr), &v->ptr);
+    if (g_exchange->view(x, v) == 0) return 1;
+    PyErr_Clear();
+    return refuse(PyExc_TypeError, name, "is not a tensor with memory of its own");
+}
+static int device_of(const View *v) { return v->device_type == ON_CUDA ? v->device : -1; }
+static int look(PyObject *x, const char *name, int want, Seen *s)
+{
+    static const uint8_t kinds[4] = {2, 4, 1, 0}, bits[4] = {32, 16, 8, 32};         /* DLPack's: float, bfloat, unsigned, signed */
+    View v;
+    if (!view(x, name, &v)) return 0;
+    for (s->type = 0; s->type < 4 && (v.kind != kinds[s->type] || v.bits != bits[s->type] || v.lanes != 1); ++s->type) { }
+    if (want < 0 ? s->type > BF16_T : s->type != want) return refuse(PyExc_TypeError, name, "has the wrong element type");
+    if (v.dims > 4) return refuse(PyExc_ValueError, name, "has the wrong shape");
+    s->dims = v.dims;
+    for (int i = 0; i < v.dims; ++i) { s->size[i] = v.size[i]; s->stride[i] = v.stride[i]; }
+    s->ptr = (char *)v.data + v.offset;
+    s->device = device_of(&v);
+    return 1;
 }
 /* memory of the CUDA device that was current when the call began (began()); what is not is reported when all else is right */
-static __thread long g_current;                      /* of this thread's call: a tensor's attributes may run Python, which lets other threads in */
+static __thread long g_current;                      /* of this thread's call: an argument may run Python, which lets other threads in */
 static __thread const char *g_elsewhere, *g_where;
 static int began(void)
 {
-    if (!torch_types()) return 0;
+    if (!torch_tensors()) return 0;
     g_elsewhere = NULL;
-    PyObject *cur = PyObject_CallNoArgs(g_get_device);
+    PyObject *cur = PyObject_CallNoArgs(g_current_device);
     g_current = cur ? PyLong_AsLong(cur) : -1;
     if (!cur) PyErr_Clear();                           /* no device: no tensor of one either */
     Py_XDECREF(cur);
     return 1;
 }
-static int here(PyObject *x, const char *name)
+static int here(int device, const char *name)
 {
-    PyObject *at = PyObject_CallMethodNoArgs(x, s_get_device);
-    const long d = at ? PyLong_AsLong(at) : -1;
-    Py_XDECREF(at);
-    if (!at || (d == -1 && PyErr_Occurred())) return 0;
-    if (!g_elsewhere && (d < 0 || d != g_current)) {
+    if (!g_elsewhere && (device < 0 || device != g_current)) {
         g_elsewhere = name;
-        g_where = d < 0 ? "is not on a CUDA device" : "is not on the current device";
+        g_where = device < 0 ? "is not on a CUDA device" : "is not on the current device";
     }
     return 1;
 }
+/* None: torch's current stream of the current device */
+static int core_stream(PyObject *x, void **out)
+{
+    return x == Py_None ? g_exchange->current_stream(ON_CUDA, (int32_t)g_current, out) == 0 : to_stream(x, out);
+}
 /* Rows: [d0, cols], or [d0, d1, cols] with d1 > 0, the rows evenly spaced and their elements adjacent. */
-static int rows_of(const Seen *v, PyObject *x, const char *name, int64_t d0, int64_t d1, int64_t cols, void **ptr, int64_t *ld)
+static int rows_of(const Seen *v, const char *name, int64_t d0, int64_t d1, int64_t cols, void **ptr, int64_t *ld)
 {
     const int lead = d1 > 0 ? 2 : 1;
     if (v->dims != lead + 1 || v->size[0] != d0 || (lead == 2 && v->size[1] != d1) || v->size[lead] != cols) return refuse(PyExc_ValueError, name, "has the wrong shape");
@@ -203,16 +225,16 @@ static int rows_of(const Seen *v, PyObject *x, const char *name, int64_t d0, int
     else *ld = d0 > 1 ? v->stride[0] : cols;
     if (!ok || *ld < cols) return refuse(PyExc_ValueError, name, "needs evenly spaced rows of adjacent elements");
     *ptr = v->ptr;
-    return here(x, name);
+    return here(v->device, name);
 }
 static int to_rows(PyObject *x, const char *name, int64_t d0, int64_t d1, int64_t cols, int type, void **ptr, int64_t *ld)      /* None is NULL */
 {
     Seen v;
     *ptr = NULL; *ld = 0;
-    return x == Py_None || (look(x, name, type, &v) && rows_of(&v, x, name, d0, d1, cols, ptr, ld));
+    return x == Py_None || (look(x, name, type, &v) && rows_of(&v, name, d0, d1, cols, ptr, ld));
 }
 /* A dense tensor of the given sizes (0 ends them). */
-static int dense_of(const Seen *v, PyObject *x, const char *name, int64_t a, int64_t b, int64_t c, void **ptr)
+static int dense_of(const Seen *v, const char *name, int64_t a, int64_t b, int64_t c, void **ptr)
 {
     const int64_t want[3] = {a, b, c};
     const int dims = c ? 3 : b ? 2 : 1;
@@ -225,25 +247,29 @@ static int dense_of(const Seen *v, PyObject *x, const char *name, int64_t a, int
         dense *= v->size[i];
     }
     *ptr = v->ptr;
-    return here(x, name);
+    return here(v->device, name);
 }
 static int to_dense(PyObject *x, const char *name, int type, int64_t a, int64_t b, int64_t c, void **ptr)                       /* None is NULL */
 {
     Seen v;
     *ptr = NULL;
-    return x == Py_None || (look(x, name, type, &v) && dense_of(&v, x, name, a, b, c, ptr));
+    return x == Py_None || (look(x, name, type, &v) && dense_of(&v, name, a, b, c, ptr));
 }
 /* Device memory of any type: its address and bytes.  None is NULL. */
 static int to_workspace(PyObject *x, void **ptr, int64_t *bytes)
 {
+    View v;
     *ptr = NULL; *bytes = 0;
     if (x == Py_None) return 1;
-    if (!torch_types()) return 0;
-    if (!PyObject_TypeCheck(x, g_tensor)) return refuse(PyExc_TypeError, "workspace", "is not a tensor");
-    PyObject *n = PyObject_GetAttr(x, s_nbytes);
-    *bytes = n ? PyLong_AsLongLong(n) : -1;
-    Py_XDECREF(n);
-    return *bytes >= 0 && to_ptr(x, ptr) && here(x, "workspace");
+    if (!view(x, "workspace", &v)) return 0;
+    int64_t dense = 1;
+    for (int i = v.dims - 1; i >= 0; --i) {
+        if (v.size[i] > 1 && v.stride[i] != dense) return not_contiguous();
+        dense *= v.size[i];
+    }
+    *ptr = (char *)v.data + v.offset;
+    *bytes = dense * (v.bits * v.lanes / 8);
+    return here(device_of(&v), "workspace");
 }
 /* A tensor of `dims` dimensions, each a positive 32-bit number: one that the others follow. */
 static int to_lead(PyObject *x, const char *name, int type, int dims, Seen *v)
@@ -377,8 +403,10 @@ FN(vtrace)
     PTR(vs, 11); PTR(pg, 12); STREAM(13);
     CALL(hts_vtrace(lr, r, v, d, b, gamma, lambda, rho, c, T, N, vs, pg, stream), "hts_vtrace");
 }
-#define CORE_CALL(expr, what) \
+#define CORE_CALL(i, expr, what) \
+    void *stream; \
     if (g_elsewhere) { refuse(PyExc_ValueError, g_elsewhere, g_where); return NULL; } \
+    if (!core_stream(a[i], &stream)) return NULL; \
     CALL(expr, what)
 #define ROWS(x, name, d0, d1, cols, ptr, ld) if (!to_rows(x, name, d0, d1, cols, dtype, (void **)&(ptr), &(ld))) return NULL
 #define DENSE(x, name, type, d0, d1, d2, ptr) if (!to_dense(x, name, type, d0, d1, d2, (void **)&(ptr))) return NULL
@@ -399,12 +427,12 @@ static PyObject *conv_like(PyObject *const *a, Py_ssize_t nargs, int form)      
     dtype = vx.type; T = lead == 2 ? vx.size[0] : 0; N = vx.size[lead - 1]; D = vx.size[lead]; W = vw.size[1];
     if (W < 2 || W > 4) { refuse(PyExc_ValueError, "w", "needs two to four taps"); return NULL; }
     const int64_t d0 = lead == 2 ? T : N, d1 = lead == 2 ? N : 0;
-    if (!rows_of(&vx, a[0], "x", d0, d1, D, &x, &d.ld_x) || !dense_of(&vw, a[1], "w", D, W, 0, (void **)&w)) return NULL;
+    if (!rows_of(&vx, "x", d0, d1, D, &x, &d.ld_x) || !dense_of(&vw, "w", D, W, 0, (void **)&w)) return NULL;
     DENSE(a[2], "bias", F32_T, D, 0, 0, bias);
     DENSE(a[3], "starts", U8_T, d0, d1, 0, starts);
     DENSE(a[4], form == 1 ? "slots" : "lengths", I32_T, N, 0, 0, index);
     if (form == 1) {
-        if (!to_lead(a[5], "window_in", dtype, 3, &vp) || !dense_of(&vp, a[5], "window_in", vp.size[0], W - 1, D, &win)) return NULL;
+        if (!to_lead(a[5], "window_in", dtype, 3, &vp) || !dense_of(&vp, "window_in", vp.size[0], W - 1, D, &win)) return NULL;
         pool = vp.size[0];
     } else
         DENSE(a[5], "window_in", dtype, N, W - 1, D, win);
@@ -418,14 +446,12 @@ static PyObject *conv_like(PyObject *const *a, Py_ssize_t nargs, int form)      
         DENSE(a[11], "dbias", F32_T, D, 0, 0, db);
         DENSE(a[12], "dwindow_in", F32_T, N, W - 1, D, dwin);
         if (!to_workspace(a[13], &work, &bytes)) return NULL;
-        STREAM(14);
-        CORE_CALL(hts_causal_conv_gradient(&d, x, w, bias, starts, index, win, dy, dwout, dx, dw, db, dwin, work, bytes, stream), "hts_causal_conv_gradient");
+        CORE_CALL(14, hts_causal_conv_gradient(&d, x, w, bias, starts, index, win, dy, dwout, dx, dw, db, dwin, work, bytes, stream), "hts_causal_conv_gradient");
     }
     ROWS(a[7], "y", d0, d1, D, y, d.ld_y);
     DENSE(a[8], "window_out", dtype, form == 1 ? pool : N, W - 1, D, wout);
-    STREAM(9);
-    if (form == 1) { CORE_CALL(hts_causal_conv_step(&d, x, w, bias, starts, index, (int32_t)pool, win, y, wout, stream), "hts_causal_conv_step"); }
-    CORE_CALL(hts_causal_conv(&d, x, w, bias, starts, index, win, y, wout, stream), "hts_causal_conv");
+    if (form == 1) { CORE_CALL(9, hts_causal_conv_step(&d, x, w, bias, starts, index, (int32_t)pool, win, y, wout, stream), "hts_causal_conv_step"); }
+    CORE_CALL(9, hts_causal_conv(&d, x, w, bias, starts, index, win, y, wout, stream), "hts_causal_conv");
 }
 FN(causal_conv) { (void)self; return conv_like(a, nargs, 0); }
 FN(causal_conv_step) { (void)self; return conv_like(a, nargs, 1); }
@@ -447,7 +473,7 @@ static PyObject *scan_like(PyObject *const *a, Py_ssize_t nargs, int form)
     if (!began() || !to_lead(a[0], "x", -1, lead + 1, &vx) || !to_lead(a[2], "a", F32_T, 2, &va)) return NULL;
     dtype = vx.type; T = lead == 2 ? vx.size[0] : 0; N = vx.size[lead - 1]; D = vx.size[lead]; S = va.size[1];
     const int64_t d0 = lead == 2 ? T : N, d1 = lead == 2 ? N : 0;
-    if (!rows_of(&vx, a[0], "x", d0, d1, D, (void **)&in.x, &d.ld_x) || !dense_of(&va, a[2], "a", D, S, 0, (void **)&in.a)) return NULL;
+    if (!rows_of(&vx, "x", d0, d1, D, (void **)&in.x, &d.ld_x) || !dense_of(&va, "a", D, S, 0, (void **)&in.a)) return NULL;
     ROWS(a[1], "dt", d0, d1, D, in.dt, d.ld_dt);
     ROWS(a[3], "b", d0, d1, S, in.b, d.ld_b);
     ROWS(a[4], "c", d0, d1, S, in.c, d.ld_c);
@@ -457,7 +483,7 @@ static PyObject *scan_like(PyObject *const *a, Py_ssize_t nargs, int form)
     DENSE(a[8], "starts", U8_T, d0, d1, 0, in.starts);
     DENSE(a[9], form == 1 ? "slots" : "lengths", I32_T, N, 0, 0, index);
     if (form == 1) {
-        if (!to_lead(a[10], "state_in", F32_T, 3, &vp) || !dense_of(&vp, a[10], "state_in", vp.size[0], D, S, (void **)&in.state_in)) return NULL;
+        if (!to_lead(a[10], "state_in", F32_T, 3, &vp) || !dense_of(&vp, "state_in", vp.size[0], D, S, (void **)&in.state_in)) return NULL;
         pool = vp.size[0];
     } else
         DENSE(a[10], "state_in", F32_T, N, D, S, in.state_in);
@@ -479,18 +505,15 @@ static PyObject *scan_like(PyObject *const *a, Py_ssize_t nargs, int form)
         DENSE(entry(a[14], "dt_bias"), "grads['dt_bias']", F32_T, D, 0, 0, g.dt_bias);
         DENSE(entry(a[14], "state_in"), "grads['state_in']", F32_T, N, D, S, g.state_in);
         if (!to_workspace(a[15], &work, &bytes)) return NULL;
-        STREAM(16);
-        CORE_CALL(hts_selective_scan_gradient(&d, &in, dy, ld_dy, dsout, &g, work, bytes, stream), "hts_selective_scan_gradient");
+        CORE_CALL(16, hts_selective_scan_gradient(&d, &in, dy, ld_dy, dsout, &g, work, bytes, stream), "hts_selective_scan_gradient");
     }
     ROWS(a[12], "y", d0, d1, D, y, d.ld_y);
     DENSE(a[13], "state_out", F32_T, form == 1 ? pool : N, D, S, sout);
     if (form == 1) {
-        STREAM(14);
-        CORE_CALL(hts_selective_scan_step(&d, &in, index, (int32_t)pool, y, sout, stream), "hts_selective_scan_step");
+        CORE_CALL(14, hts_selective_scan_step(&d, &in, index, (int32_t)pool, y, sout, stream), "hts_selective_scan_step");
     }
     if (!to_workspace(a[14], &work, &bytes)) return NULL;
-    STREAM(15);
-    CORE_CALL(hts_selective_scan(&d, &in, y, sout, work, bytes, stream), "hts_selective_scan");
+    CORE_CALL(15, hts_selective_scan(&d, &in, y, sout, work, bytes, stream), "hts_selective_scan");
 }
 FN(selective_scan) { (void)self; return scan_like(a, nargs, 0); }
 FN(selective_scan_step) { (void)self; return scan_like(a, nargs, 1); }
@@ -508,16 +531,15 @@ FN(linear)
     const int32_t dtype = BF16_T;
     if (!began() || !to_lead(a[0], "x", dtype, 2, &vx) || !to_lead(a[1], "w", dtype, 2, &vw)) return NULL;
     M = vx.size[0]; K = vx.size[1]; N = vw.size[0];
-    if (!rows_of(&vx, a[0], "x", M, 0, K, &x, &d.ld_x) || !dense_of(&vw, a[1], "w", N, K, 0, &w)) return NULL;
+    if (!rows_of(&vx, "x", M, 0, K, &x, &d.ld_x) || !dense_of(&vw, "w", N, K, 0, &w)) return NULL;
     DENSE(a[2], "bias", F32_T, N, 0, 0, bias);
     ROWS(a[3], "residual", M, 0, N, res, d.ld_residual);
     I32(act, 4);
     ROWS(a[5], "y", M, 0, N, y, d.ld_y);
     ROWS(a[6], "pre", M, 0, N, pre, d.ld_pre);
     if (!to_workspace(a[7], &work, &bytes)) return NULL;
-    STREAM(8);
     d.rows = (int32_t)M; d.in_features = (int32_t)K; d.out_features = (int32_t)N; d.activation = act;
-    CORE_CALL(hts_linear(&d, x, w, bias, res, y, pre, work, bytes, stream), "hts_linear");
+    CORE_CALL(8, hts_linear(&d, x, w, bias, res, y, pre, work, bytes, stream), "hts_linear");
 }
 FN(linear_gradient)
 {
@@ -531,7 +553,7 @@ FN(linear_gradient)
     const int32_t dtype = BF16_T;
     if (!began() || !to_lead(a[0], "x", dtype, 2, &vx) || !to_lead(a[1], "w", dtype, 2, &vw)) return NULL;
     M = vx.size[0]; K = vx.size[1]; N = vw.size[0];
-    if (!rows_of(&vx, a[0], "x", M, 0, K, &x, &d.ld_x) || !dense_of(&vw, a[1], "w", N, K, 0, &w)) return NULL;
+    if (!rows_of(&vx, "x", M, 0, K, &x, &d.ld_x) || !dense_of(&vw, "w", N, K, 0, &w)) return NULL;
     ROWS(a[2], "pre", M, 0, N, pre, d.ld_pre);
     ROWS(a[3], "dy", M, 0, N, dy, d.ld_dy);
     I32(act, 4);
@@ -544,9 +566,8 @@ FN(linear_gradient)
     }
     DENSE(a[7], "dbias", F32_T, N, 0, 0, db);
     if (!to_workspace(a[8], &work, &bytes)) return NULL;
-    STREAM(9);
     d.rows = (int32_t)M; d.in_features = (int32_t)K; d.out_features = (int32_t)N; d.activation = act;
-    CORE_CALL(hts_linear_gradient(&d, x, w, pre, dy, dx, dw, db, work, bytes, stream), "hts_linear_gradient");
+    CORE_CALL(9, hts_linear_gradient(&d, x, w, pre, dy, dx, dw, db, work, bytes, stream), "hts_linear_gradient");
 }
 
 static PyObject *init(PyObject *self, PyObject *error)
@@ -569,11 +590,6 @@ PyMODINIT_FUNC PyInit__native(void)
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
     s_value = PyUnicode_InternFromString("value");
-    s_dtype = PyUnicode_InternFromString("dtype");
-    s_shape = PyUnicode_InternFromString("shape");
-    s_stride = PyUnicode_InternFromString("stride");
-    s_get_device = PyUnicode_InternFromString("get_device");
-    s_nbytes = PyUnicode_InternFromString("nbytes");
     for (int i = 0; i < 12; ++i) s_weights[i] = PyUnicode_InternFromString(kWeights[i]);
     PyObject *np = PyImport_ImportModule("numpy"), *ct = np ? PyImport_ImportModule("ctypes") : NULL;
     g_ndarray = np ? (PyTypeObject *)PyObject_GetAttrString(np, "ndarray") : NULL;

@@ -71,3 +71,13 @@ def within(got, ref, slack, what=""):
     room = HALF_STEP[got.dtype] * ref.abs() + slack
     worst = (err - room).max()
     assert bool(torch.isfinite(got.float()).all()) and float(worst) <= 0, f"{what}: beyond its bound by {float(worst):.3g}, largest error {float(err.max()):.3g}"
+
+
+def lend(stream, *tensors):
+    """Tensors of the current stream for a call on another: what fills them comes first, and their memory goes to nobody else before the call is done."""
+    if stream is not None:
+        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+        s.wait_stream(torch.cuda.current_stream())
+        for t in tensors:
+            if t is not None:
+                t.record_stream(s)

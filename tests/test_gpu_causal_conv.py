@@ -33,6 +33,7 @@ def outputs(c, sentinel=7.0):
 
 def run(c, act, stream=None):
     y, out = outputs(c)
+    ref.lend(stream, y, out)
     hts.hts_causal_conv(c["x"], c["w"], c["bias"], c["starts"], c["lengths"], c["window_in"], act, y, out, stream)
     return y, out
 
@@ -130,6 +131,7 @@ def gradient(c, act, dy, dout, want=("dx", "dw", "dbias", "dwindow_in"), stream=
          "dwindow_in": torch.empty(N, W - 1, D, device="cuda")}
     o = {k: v if k in want else None for k, v in o.items()}
     work = torch.empty(hts.hts_causal_conv_workspace(T, N, D, W), dtype=torch.uint8, device="cuda")
+    ref.lend(stream, work, *o.values())
     hts.hts_causal_conv_gradient(c["x"], c["w"], c["bias"], c["starts"], c["lengths"], c["window_in"], act, dy, dout, o["dx"], o["dw"], o["dbias"], o["dwindow_in"], work,
                                  stream)
     return o

@@ -27,6 +27,7 @@ def run(c, act, keep=False, y=None, stream=None):
     y = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda") if y is None else y
     pre = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda") if keep else None
     work = torch.empty(hts.hts_linear_workspace(M, K, N), dtype=torch.uint8, device="cuda")
+    ref.lend(stream, y, pre, work)
     hts.hts_linear(c["x"], c["w"], c["bias"], c["residual"], act, y, pre, work, stream)
     return y, pre
 
@@ -89,6 +90,7 @@ def gradient(c, act, pre, dy, dw_type=torch.float32, want=("dx", "dw", "dbias"),
     o = {"dx": torch.full((M, K), 7.0, dtype=torch.bfloat16, device="cuda"), "dw": torch.full((N, K), 7.0, dtype=dw_type, device="cuda"), "dbias": torch.full((N,), 7.0, device="cuda")}
     o = {k: v if k in want else None for k, v in o.items()}
     work = torch.empty(hts.hts_linear_workspace(M, K, N, True), dtype=torch.uint8, device="cuda")
+    ref.lend(stream, work, *o.values())
     hts.hts_linear_gradient(c["x"], c["w"], pre, dy, act, o["dx"], o["dw"], o["dbias"], work, stream)
     return o
 

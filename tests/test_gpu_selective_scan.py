@@ -31,6 +31,7 @@ def run(c, stream=None):
     y = torch.full((T, N, D), 7.0, dtype=c["x"].dtype, device="cuda")
     out = torch.full((N, D, S), 7.0, device="cuda")
     work = torch.empty(hts.hts_selective_scan_workspace(T, N, D, S), dtype=torch.uint8, device="cuda")
+    ref.lend(stream, y, out, work)
     hts.hts_selective_scan(**c, y=y, state_out=out, workspace=work, stream=stream)
     return y, out
 
@@ -181,6 +182,7 @@ def gradient(c, dy, dout, want=None, stream=None):
     if want:
         o = {k: o[k] for k in want}
     work = torch.empty(hts.hts_selective_scan_workspace(T, N, D, c["a"].shape[1], True), dtype=torch.uint8, device="cuda")
+    ref.lend(stream, work, *o.values())
     hts.hts_selective_scan_gradient(**c, dy=dy, dstate_out=dout, grads=o, workspace=work, stream=stream)
     return o
 

@@ -162,24 +162,56 @@ def test_a_size_that_a_call_refuses_has_no_workspace():
         assert scan_call(**sizes, bytes=1 << 60) == INVALID
 
 
+def scan_tensors(**kw):
+    z = torch.zeros
+    return {**dict(x=z(4, 2, 8), dt=z(4, 2, 8), a=z(8, 16), b=z(4, 2, 16), c=z(4, 2, 16), d=None, dt_bias=None, z=None, starts=None, lengths=None, state_in=None, softplus=True, y=z(4, 2, 8),
+                   state_out=None, workspace=None, stream=0), **kw}
+
+
 def test_threads_do_not_see_each_others_tensors():
-    """A tensor whose attributes run Python lets another thread's call in between the checks of this one, which reports its own first fault all the same."""
+    """An argument that runs Python lets another thread's call in between the checks of this one, which reports its own first fault all the same."""
     import threading
     calls = []
 
-    class Slow(torch.Tensor):
-        @classmethod
-        def __torch_function__(cls, func, types, args=(), kwargs=None):
-            if getattr(func, "__name__", "") == "stride":
-                def other():
-                    with pytest.raises(TypeError):
-                        hts.hts_causal_conv(**conv_tensors(x=5))
-                    calls.append(1)
-                t = threading.Thread(target=other)
-                t.start()
-                t.join()
-            return super().__torch_function__(func, types, args, kwargs or {})
+    class Slow:
+        def __bool__(self):
+            def other():
+                with pytest.raises(TypeError):
+                    hts.hts_causal_conv(**conv_tensors(x=5))
+                calls.append(1)
+            t = threading.Thread(target=other)
+            t.start()
+            t.join()
+            return True
 
     with pytest.raises(ValueError, match="x is not on a CUDA device"):
-        hts.hts_causal_conv(**conv_tensors(window_out=torch.zeros(2, 3, 8).as_subclass(Slow)))
+        hts.hts_selective_scan(**scan_tensors(softplus=Slow()))
     assert calls
+
+
+@pytest.mark.parametrize("x,error", [(torch.zeros(4, 2, 8, device="meta"), "x is not"), (torch.zeros(4, 2, 8).to_sparse(), "x is not a tensor with memory"),
+                                     (torch.zeros(4, 2, 8, dtype=torch.complex64), "element type"), (torch.zeros(4, 2, 8, dtype=torch.bool), "element type"),
+                                     (torch.zeros(4, 2, 8, dtype=torch.int32), "element type"), (torch.zeros(4, 2, 8, dtype=torch.float64), "element type"),
+                                     (torch.zeros(1, 1, 4, 2, 8), "shape"), (torch.zeros(()), "shape"), (torch.nn.Parameter(torch.zeros(4, 2, 8)), "x is not on a CUDA device"),
+                                     (torch.zeros(4, 2, 16)[..., 3:11], "x is not on a CUDA device")])
+def test_tensors_of_other_kinds(x, error):
+    with pytest.raises((TypeError, ValueError), match=error):
+        hts.hts_selective_scan(**scan_tensors(x=x))
+    with pytest.raises((TypeError, ValueError), match="workspace is not|must be|x is not"):
+        hts.hts_selective_scan(**scan_tensors(workspace="0"))
+
+
+def test_workspaces_are_contiguous():
+    with pytest.raises(AssertionError):
+        hts.hts_selective_scan(**scan_tensors(workspace=torch.zeros(64, 2)[:, 0]))
+
+
+def test_references_are_kept():
+    """A refused call and its checks leave no reference behind and take none away."""
+    import sys
+    t = scan_tensors()
+    before = {k: sys.getrefcount(v) for k, v in t.items() if isinstance(v, torch.Tensor)}
+    for _ in range(100):
+        with pytest.raises(ValueError):
+            hts.hts_selective_scan(**t)
+    assert before == {k: sys.getrefcount(v) for k, v in t.items() if isinstance(v, torch.Tensor)}
