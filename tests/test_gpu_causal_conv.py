@@ -224,3 +224,25 @@ def test_captured_calls_replay_and_other_streams():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want_y) and torch.equal(out, want_out) and all(torch.equal(o[k], want[k]) for k in o)
+
+
+@pytest.mark.parametrize("type", TYPES)
+@pytest.mark.parametrize("W", [2, 3, 4])
+def test_weights_that_start_anywhere(W, type):
+    c = case(40, 3, 24, W, type=type)
+    dy = torch.randn_like(c["x"])
+    want, want_g = run(c, "silu"), gradient(c, "silu", dy, None)
+    for off in (1, 2):
+        moved = dict(c)
+        for k in ("w", "bias"):
+            room = torch.zeros(c[k].numel() + off, device="cuda")
+            moved[k] = room[off:].view(c[k].shape).copy_(c[k])
+        got, got_g = run(moved, "silu"), gradient(moved, "silu", dy, None)
+        assert all(torch.equal(u, v) for u, v in zip(got, want))
+        assert torch.equal(got_g["dx"], want_g["dx"]) and all(ref.rel2(got_g[k], want_g[k].double()) <= 120 * 2.0 ** -24 for k in ("dw", "dbias"))      # 120 steps, in another order
+        row, rows = torch.empty_like(c["x"][0]), torch.empty_like(want[1])
+        other, others = torch.empty_like(row), torch.empty_like(rows)
+        window = torch.zeros_like(want[1]) if c["window_in"] is None else c["window_in"]
+        hts.hts_causal_conv_step(c["x"][0], c["w"], c["bias"], None, None, window, "silu", row, rows)
+        hts.hts_causal_conv_step(c["x"][0], moved["w"], moved["bias"], None, None, window, "silu", other, others)
+        assert torch.equal(row, other) and torch.equal(rows, others)
