@@ -31,6 +31,7 @@ struct ScanArgs {
     const uint8_t* starts;
     const int32_t* lengths;
     bool softplus;
+    bool fours;                                 // states, A and their gradients may be moved in fours: S is a multiple, all start on 16-byte boundaries
 };
 // The runs' maps: ends [run][N][D][S] (overwritten by the runs' first states), sums of delta [run][N][D], whether a run has a
 // start [run][N].  The gradient's: what a run hands back of its own outputs' gradients [run][N][D][S].
@@ -103,36 +104,56 @@ __device__ __forceinline__ uint8_t start_at(const ScanArgs& p, int n, int t, int
     return p.starts && lane < 8 && at < end ? p.starts[(size_t)at * p.N + n] : 0;
 }
 
-// SP states of A, times log2(e), as pairs; zero behind the last state.
+// SP adjacent numbers of which `left` exist, zero behind them; four at once if they may be (ScanArgs::fours).  Neighbouring lanes' states lie
+// S numbers apart, so that one at a time takes a sector of its own for each: 16 loads and stores of 32 sectors a warp (a rollout of 128 steps
+// 231 us, in fours 216).
 template <int SP>
-__device__ __forceinline__ void load_decays(const ScanArgs& p, int ch, int s0, bool on, f32x2 (&a2)[SP / 2])
+__device__ __forceinline__ void load_states(const float* from, bool on, int left, bool fours, f32x2 (&h)[SP / 2])
 {
+    float v[SP];
 #pragma unroll
-    for (int i = 0; i < SP / 2; ++i) {
-        float v[2];
+    for (int i = 0; i < SP; i += 4) {
+        Vec<float, 4> q{};
+        if (fours) {
+            if (on && i < left) q = load_vec<4>(from + i);
+        } else
 #pragma unroll
-        for (int k = 0; k < 2; ++k) v[k] = on && s0 + 2 * i + k < p.S ? p.a[(size_t)ch * p.S + s0 + 2 * i + k] * kLog2e : 0.f;
-        a2[i] = pair(v[0], v[1]);
+            for (int k = 0; k < 4; ++k)
+                if (on && i + k < left) q.v[k] = from[i + k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[i + k] = q.v[k];
     }
+#pragma unroll
+    for (int i = 0; i < SP / 2; ++i) h[i] = pair(v[2 * i], v[2 * i + 1]);
 }
 // The states from s0 of a channel, [..][D][S].
 template <int SP>
 __device__ __forceinline__ void load_states(const ScanArgs& p, const float* from, size_t row, int ch, int s0, bool on, f32x2 (&h)[SP / 2])
 {
-#pragma unroll
-    for (int i = 0; i < SP / 2; ++i) {
-        float v[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) v[k] = from && on && s0 + 2 * i + k < p.S ? from[(row * p.D + ch) * p.S + s0 + 2 * i + k] : 0.f;
-        h[i] = pair(v[0], v[1]);
-    }
+    load_states<SP>(from + (row * p.D + ch) * p.S + s0, from && on, p.S - s0, p.fours, h);
 }
 template <int SP>
-__device__ __forceinline__ void store_states(const ScanArgs& p, float* to, size_t row, int ch, int s0, bool on, const f32x2 (&h)[SP / 2])
+__device__ __forceinline__ void store_states(const ScanArgs& p, float* to, size_t row, int ch, int s0, bool on, const f32x2 (&h)[SP / 2], bool fours)
 {
+    to += (row * p.D + ch) * p.S + s0;
 #pragma unroll
-    for (int i = 0; i < SP; ++i)
-        if (on && s0 + i < p.S) to[(row * p.D + ch) * p.S + s0 + i] = lane_of(h[i / 2], i & 1);
+    for (int i = 0; i < SP; i += 4) {
+        const float v[4] = {lane_of(h[i / 2], 0), lane_of(h[i / 2], 1), lane_of(h[i / 2 + 1], 0), lane_of(h[i / 2 + 1], 1)};
+        if (fours) {
+            if (on && s0 + i < p.S) store_vec<4>(to + i, v);
+        } else
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (on && s0 + i + k < p.S) to[i + k] = v[k];
+    }
+}
+// SP states of A, times log2(e), as pairs.
+template <int SP>
+__device__ __forceinline__ void load_decays(const ScanArgs& p, int ch, int s0, bool on, f32x2 (&a2)[SP / 2])
+{
+    load_states<SP>(p, p.a, 0, ch, s0, on, a2);
+#pragma unroll
+    for (int i = 0; i < SP / 2; ++i) a2[i] = mul2(a2[i], both(kLog2e));
 }
 // Steps t .. t + ROWS - 1 of sequence n, channels c0 .. c0 + CB - 1, to shared memory; zeros behind the last step and channel.  WIDE: by
 // asynchronous copies of 16 bytes (rows and channels start on such boundaries), else element by element.
@@ -156,8 +177,9 @@ __device__ __forceinline__ void copy_rows(const ScanArgs& p, T (*to)[CB], const 
 enum Mode { SCAN, MAPS, MAPS_BACK };            // outputs; the runs' maps; those and what the runs hand back
 
 // SPT states a thread, LS lanes a channel.  dy: MAPS_BACK only, in the place of y.
+// Blocks of an SM: with five MAPS_BACK has no registers for its two further values a state (gradient of 2047 x 2 steps 170 us, with four 154).
 template <typename T, int SPT, int LS, Mode MODE, bool WIDE>
-__global__ void __launch_bounds__(kThreads, 5) scan_kernel(const ScanArgs p, const T* x, const T* dt, const T* b, const T* c, const T* z, const T* dy, const float* first,
+__global__ void __launch_bounds__(kThreads, MODE == MAPS_BACK ? 4 : 5) scan_kernel(const ScanArgs p, const T* x, const T* dt, const T* b, const T* c, const T* z, const T* dy, const float* first,
                                                         T* y, float* state_out, RunMaps m)
 {
     constexpr int SP = SPT * LS, CB = kThreads / LS;
@@ -279,11 +301,11 @@ __global__ void __launch_bounds__(kThreads, 5) scan_kernel(const ScanArgs p, con
         if (++stage == kStages) stage = 0;
     }
     if (MODE == SCAN) {
-        if (state_out && run == p.runs - 1) store_states<SPT>(p, state_out, n, ch, s0, on, h);
+        if (state_out && run == p.runs - 1) store_states<SPT>(p, state_out, n, ch, s0, on, h, p.fours);
     } else {
         const size_t row = (size_t)run * p.N + n;
-        store_states<SPT>(p, m.ends, row, ch, s0, on, h);
-        if (MODE == MAPS_BACK) store_states<SPT>(p, m.back, row, ch, s0, on, back);
+        store_states<SPT>(p, m.ends, row, ch, s0, on, h, p.fours);
+        if (MODE == MAPS_BACK) store_states<SPT>(p, m.back, row, ch, s0, on, back, p.fours);
         if (on && sub == 0) m.sums[row * p.D + ch] = sum;
         if (threadIdx.x == 0) m.broken[row] = broken;       // the same from every block of the row
     }
@@ -688,8 +710,8 @@ __global__ void __launch_bounds__(kThreads, 3) scan_gradient_kernel(const ScanAr
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         const bool on = c0 + e < p.D;
-        if (run == 0 && q.dstate_in) store_states<4>(p, q.dstate_in, n, on ? c0 + e : 0, s0, on, carry[e]);
-        if (q.part_ch) store_states<4>(p, q.part_ch + row0 * ((size_t)p.D * p.S + 2 * p.D), 0, on ? c0 + e : 0, s0, on, da[e]);
+        if (run == 0 && q.dstate_in) store_states<4>(p, q.dstate_in, n, on ? c0 + e : 0, s0, on, carry[e], p.fours);
+        if (q.part_ch) store_states<4>(p, q.part_ch + row0 * ((size_t)p.D * p.S + 2 * p.D), 0, on ? c0 + e : 0, s0, on, da[e], p.fours && p.D % 2 == 0);
     }
     if (q.part_ch) {
         float *part = q.part_ch + row0 * ((size_t)p.D * p.S + 2 * p.D), *sums = &sh.gb[0][0];       // kChunk CB of them, kThreads at least
@@ -804,11 +826,14 @@ RunMaps maps_at(const Plan& q, void* workspace)
     char* w = (char*)workspace;
     return {(float*)(w + q.ends), (float*)(w + q.sums), (float*)(w + q.back), (uint8_t*)(w + q.broken)};
 }
-ScanArgs scan_args(const hts_scan_desc& d, const hts_scan_inputs& in)
+// states: other tensors of states that the call reads or writes
+ScanArgs scan_args(const hts_scan_desc& d, const hts_scan_inputs& in, std::initializer_list<const void*> states)
 {
     ScanArgs p{};
     p.T = d.T; p.N = d.N; p.D = d.channels; p.S = d.state; p.runs = 1; p.length = d.T;
     p.ld_x = d.ld_x; p.ld_dt = d.ld_dt; p.ld_b = d.ld_b; p.ld_c = d.ld_c; p.ld_z = d.ld_z; p.ld_y = d.ld_y;
+    p.fours = d.state % 4 == 0;
+    for (const void* q : states) p.fours = p.fours && aligned_to(q, 16);
     p.a = in.a; p.d = in.d; p.dt_bias = in.dt_bias; p.starts = in.starts; p.lengths = in.lengths; p.softplus = d.softplus != 0;
     return p;
 }
@@ -963,7 +988,7 @@ extern "C" hts_status hts_selective_scan(const hts_scan_desc* d, const hts_scan_
     if (bad(d, in, true) || !y || d->ld_y < d->channels || far(d->N, {d->ld_y}) || y == in->x || y == in->dt || y == in->z || (state_out && state_out == in->state_in)) return HTS_ERR_INVALID_ARG;
     const int64_t need = hts_selective_scan_workspace(d->T, d->N, d->channels, d->state, 0);
     if (need && (!workspace || !aligned_to(workspace, 16) || workspace_bytes < need)) return HTS_ERR_INVALID_ARG;
-    const ScanArgs p = scan_args(*d, *in);
+    const ScanArgs p = scan_args(*d, *in, {in->a, in->state_in, state_out});
     if (d->dtype == HTS_DTYPE_FP32) return forward(p, *in, (float*)y, state_out, workspace, (cudaStream_t)stream);
     return forward(p, *in, (__nv_bfloat16*)y, state_out, workspace, (cudaStream_t)stream);
 }
@@ -973,7 +998,7 @@ extern "C" hts_status hts_selective_scan_step(const hts_scan_desc* d, const hts_
     if (bad(d, in, false) || !y || !in->state_in || !state_out || in->lengths || d->ld_y < d->channels || y == in->x || y == in->dt || y == in->z || pool < 1 ||
         (!slots && pool < d->N))
         return HTS_ERR_INVALID_ARG;
-    const ScanArgs p = scan_args(*d, *in);
+    const ScanArgs p = scan_args(*d, *in, {in->a, in->state_in, state_out});
     if (d->dtype == HTS_DTYPE_FP32) return step(p, *in, slots, pool, (float*)y, state_out, (cudaStream_t)stream);
     return step(p, *in, slots, pool, (__nv_bfloat16*)y, state_out, (cudaStream_t)stream);
 }
@@ -988,7 +1013,7 @@ extern "C" hts_status hts_selective_scan_gradient(const hts_scan_desc* d, const 
     for (const void* o : {out->x, out->dt, out->z, out->b, out->c})
         if (o && (o == in->x || o == in->dt || o == in->z || o == in->b || o == in->c || o == dy)) return HTS_ERR_INVALID_ARG;
     if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < hts_selective_scan_workspace(d->T, d->N, d->channels, d->state, 1)) return HTS_ERR_INVALID_ARG;
-    const ScanArgs p = scan_args(*d, *in);
+    const ScanArgs p = scan_args(*d, *in, {in->a, in->state_in, dstate_out, out->state_in});
     if (d->dtype == HTS_DTYPE_FP32) return gradient(p, *in, (const float*)dy, ld_dy, dstate_out, *out, workspace, (cudaStream_t)stream);
     return gradient(p, *in, (const __nv_bfloat16*)dy, ld_dy, dstate_out, *out, workspace, (cudaStream_t)stream);
 }
