@@ -781,15 +781,6 @@ hts_status by_gradient_lanes(int S, F f)
     }
 }
 
-// Runs so that `blocks` blocks exist, of `least` steps at least and a multiple of the steps staged at once.
-void cut_runs(int T, int64_t base, int64_t blocks, int least, int* runs, int* length)
-{
-    const int64_t want = ceil_div(blocks, base);
-    int64_t l = ceil_div(ceil_div(T, want), kGroup) * kGroup;
-    if (l < least) l = least;
-    *runs = (int)ceil_div(T, l);
-    *length = *runs == 1 ? T : (int)l;
-}
 int64_t channel_blocks(int D, Shape h) { return ceil_div(D, kThreads / h.ls); }
 
 struct Plan {
@@ -797,12 +788,39 @@ struct Plan {
     int runs, length, chunks;
     size_t ends, sums, back, broken, checks, part_bc, part_ch, bytes;           // offsets in the workspace
 };
+// A step's time where each SM has its share of `blocks`, `slots` at once: alone + k with k blocks of an SM under way, more of them half in
+// rounds and half as they come.
+double step_time(double alone, int64_t blocks, int slots)
+{
+    const int64_t each = ceil_div(blocks, kCoreSms), rest = each % slots;
+    if (each <= slots) return alone + each;
+    return 0.5 * (alone + slots) * ((double)blocks / (kCoreSms * slots) + each / slots) + (rest ? 0.5 * (alone + rest) : 0);
+}
+// Runs of a sequence, or one.  Measured at 16 states, in units of 0.09 us (what one more block of an SM adds to a step): a step of the scan
+// with k <= 5 blocks an SM takes 2 + k (0.27 us alone, 0.61 with five), with 64 states or four the same within a third; the gradient's with
+// k <= 3 1.55 (3.6 + k) (0.65, 0.93).  Cut, the steps are scanned 1.8 times, or taken by the backward maps and the gradient; launches and composing take
+// 50 + 2 a run.  So few sequences are cut (4095 x 3 steps of 1024 channels: 163 us for 1030), while those that fill each SM with
+// one block or more are not (1000 x 64: 560 us, in three runs 643).
+void cut_runs(int T, int64_t base, int64_t scan_base, bool gradient, int* runs, int* length)
+{
+    double best = gradient ? T * 1.55 * step_time(3.6, base, 3) : T * step_time(2, base, 5);
+    *runs = 1;
+    *length = T;
+    for (int m = 1; m <= 12; ++m) {             // blocks of an SM
+        int64_t l = ceil_div(ceil_div(T, m * kCoreSms / base > 1 ? m * kCoreSms / base : 1), kGroup) * kGroup;
+        if (l < 4 * kGroup) l = 4 * kGroup;
+        const int64_t r = ceil_div(T, l);
+        if (r == 1 || r == *runs) continue;
+        const double time = l * (gradient ? 1.55 * step_time(3.6, base * r, 3) + 1.2 * step_time(2, scan_base * r, 4) : 1.8 * step_time(2, base * r, 5)) + 50 + 2 * r;
+        if (time < best) { best = time; *runs = (int)r; *length = (int)l; }
+    }
+}
 Plan plan(int T, int N, int D, int S, bool gradient)
 {
     Plan q{};
     const int ls = gradient_lanes(S);
     q.across = gradient ? ceil_div(D, 2 * kThreads / ls) : channel_blocks(D, scan_shape(S));
-    cut_runs(T, q.across * N, (int64_t)kCoreSms * (gradient ? 6 : 8), gradient ? 4 * kChunk : 4 * kGroup, &q.runs, &q.length);
+    cut_runs(T, q.across * N, channel_blocks(D, scan_shape(S)) * N, gradient, &q.runs, &q.length);
     size_t at = 0;
     auto take = [&](size_t floats) { const size_t was = at; at += round256(floats * 4); return was; };
     const size_t states = (size_t)N * D * S;
