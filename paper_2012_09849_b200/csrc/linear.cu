@@ -533,9 +533,11 @@ linear_split_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_consta
     }
     __syncthreads();
     cluster_sync();
-    // eight columns of a row to a thread, the cluster's partial sums in rank order
-    const int rows = min(128, o.rows - m0);
-    for (int e = rank * kSplitThreads + threadIdx.x; e < rows * (SN / 8); e += ranks * kSplitThreads) {
+    // eight columns of a row to a thread, the cluster's partial sums in rank order; as many rows to every rank, since what one SM can
+    // take from the others is what bounds this (16 x 1024 -> 512: 5.1 us where the first ranks
+    // took what 192 threads can, now 4.5)
+    const int rows = min(128, o.rows - m0), each = (rows + ranks - 1) / ranks * (SN / 8), stop = min((rank + 1) * each, rows * (SN / 8));
+    for (int e = rank * each + threadIdx.x; e < stop; e += kSplitThreads) {
         const int row = e / (SN / 8), c = e % (SN / 8) * 8;
         float v[8] = {}, bias[8];
         float4 part[8][2];
@@ -711,15 +713,16 @@ hts_status launch_split(const Operand& a, const Operand& b, int M, int N, int K,
     return HTS_OK;
 }
 // What bounds a product of few tiles is the copies into each SM: rows and columns of its blocks of k, one tile after the other, and about
-// what 1500 of them take to begin and to end (measured: 2 us).  The least of three: tiles of 128 x 64, of 128 x 128, and pairs
-// (256 rows and columns each).  Against always taking one of them, us: 16 x 1024 -> 512 6.2 (64: 6.2, 128: 6.5), 64 x 4096 -> 4096 12.7 (64:
-// 16.2, pairs: 27), 256 x 1024 -> 2048 9.1 (128: 10.6, pairs: 12.3), 1024 x 4096 -> 512 14.4 (64: 17), 4096 x 512 -> 512 8.6 (64: 10.3),
+// what 1500 of them take to begin and to end (measured: 2 us); in a cluster also the rows that an SM takes from the others, sixteen sums counted as one
+// (256 x 1024 -> 2048 without that: 9.7 us in 128 x 128 tiles, 8.2 in 128 x 64).  The least of three: tiles of 128 x 64, of 128 x 128, and pairs
+// (256 rows and columns each).  Against always taking one of them, us: 64 x 4096 -> 4096 12.7 (64:
+// 16.2, pairs: 27), 1024 x 4096 -> 512 14.4 (64: 17), 4096 x 512 -> 512 8.6 (64: 10.3),
 // 32768 x 512 -> 64 11.7 (64: 16.9).
 int64_t split_cost(int M, int N, int blocks, int SN)
 {
     const int64_t tiles = ceil_div(M, 128) * ceil_div(N, SN);
     const int ranks = split_ranks(tiles, blocks);
-    return ceil_div(tiles * ranks, kCoreSms) * (ceil_div(blocks, ranks) * (128 + SN) + 1500);
+    return ceil_div(tiles * ranks, kCoreSms) * (ceil_div(blocks, ranks) * (128 + SN) + 1500 + (ranks > 1 ? (M < 128 ? M : 128) * SN / 16 : 0));
 }
 template <bool B_ROWS, Epilogue EPI>
 hts_status launch_product(const Operand& a, const Operand& b, int M, int N, int K, const Output& o, cudaStream_t s)
