@@ -576,7 +576,8 @@ __global__ void __launch_bounds__(256) pack_kernel(const bf16* from, int64_t ld,
 }
 
 // dz = dy act'(pre), rounded (with `low`, what the rounding left out, rounded, in a second plane), and its sums over 64 rows:
-// part[row block][cols].  V channels a thread.
+// part[row block][cols].  V channels a thread: four, as eight (more registers, fewer threads) take as long for SiLU (65 us with dbias alone, 32768 x 2048)
+// and longer for ReLU and small batches.  One where rows are not aligned: eight rows at once 107 us, one after the other 212.
 constexpr int kSumRows = 64;
 template <int V>
 __global__ void __launch_bounds__(256) dz_kernel(const bf16* dy, int64_t ld_dy, const bf16* pre, int64_t ld_pre, int rows, int cols, int act, bf16* dz, int ld_dz,
@@ -587,28 +588,33 @@ __global__ void __launch_bounds__(256) dz_kernel(const bf16* dy, int64_t ld_dy, 
     __shared__ float sums[8][32 * V];
     const int across = (cols + 32 * V - 1) / (32 * V), c = (int)(blockIdx.x % across) * 32 * V + threadIdx.x * V, block = blockIdx.x / across;
     float sum[V] = {};
+    constexpr int AHEAD = V == 1 ? 8 : 4;       // rows whose loads are under way at once
     if (c < cols)
-#pragma unroll 4
-        for (int i = threadIdx.y; i < kSumRows; i += 8) {
-            const int64_t row = (int64_t)block * kSumRows + i;
-            if (row >= rows) break;
-            const Vec<bf16, V> g = load_vec<V>(dy + row * ld_dy + c);
-            float v[V];
+#pragma unroll 1
+        for (int i0 = threadIdx.y; i0 < kSumRows; i0 += 8 * AHEAD) {
+            Vec<bf16, V> g[AHEAD], u[AHEAD];
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = to_float(g.v[k]);
-            if (pre) {
-                const Vec<bf16, V> u = load_vec<V>(pre + row * ld_pre + c);
-#pragma unroll
-                for (int k = 0; k < V; ++k) v[k] = through(v[k], to_float(u.v[k]), act);
+            for (int a = 0; a < AHEAD; ++a) {   // behind the last row that one again
+                const int64_t row = min((int64_t)block * kSumRows + i0 + 8 * a, (int64_t)rows - 1);
+                g[a] = load_vec<V>(dy + row * ld_dy + c);
+                if (pre) u[a] = load_vec<V>(pre + row * ld_pre + c);
             }
 #pragma unroll
-            for (int k = 0; k < V; ++k) sum[k] += v[k];
-            if (dz) {
-                store_vec<V>(dz + row * ld_dz + c, v);
-                if (low) {
+            for (int a = 0; a < AHEAD; ++a) {
+                const int64_t row = (int64_t)block * kSumRows + i0 + 8 * a;
+                if (row >= rows) break;
+                float v[V];
 #pragma unroll
-                    for (int k = 0; k < V; ++k) v[k] = fabsf(v[k]) < INFINITY ? v[k] - to_float(from_float<bf16>(v[k])) : 0.f;
-                    store_vec<V>(dz + (rows + row) * ld_dz + c, v);
+                for (int k = 0; k < V; ++k) v[k] = pre ? through(to_float(g[a].v[k]), to_float(u[a].v[k]), act) : to_float(g[a].v[k]);
+#pragma unroll
+                for (int k = 0; k < V; ++k) sum[k] += v[k];
+                if (dz) {
+                    store_vec<V>(dz + row * ld_dz + c, v);
+                    if (low) {
+#pragma unroll
+                        for (int k = 0; k < V; ++k) v[k] = fabsf(v[k]) < INFINITY ? v[k] - to_float(from_float<bf16>(v[k])) : 0.f;
+                        store_vec<V>(dz + (rows + row) * ld_dz + c, v);
+                    }
                 }
             }
         }
@@ -715,9 +721,8 @@ hts_status launch_split(const Operand& a, const Operand& b, int M, int N, int K,
 // What bounds a product of few tiles is the copies into each SM: rows and columns of its blocks of k, one tile after the other, and about
 // what 1500 of them take to begin and to end (measured: 2 us); in a cluster also the rows that an SM takes from the others, sixteen sums counted as one
 // (256 x 1024 -> 2048 without that: 9.7 us in 128 x 128 tiles, 8.2 in 128 x 64).  The least of three: tiles of 128 x 64, of 128 x 128, and pairs
-// (256 rows and columns each).  Against always taking one of them, us: 64 x 4096 -> 4096 12.7 (64:
-// 16.2, pairs: 27), 1024 x 4096 -> 512 14.4 (64: 17), 4096 x 512 -> 512 8.6 (64: 10.3),
-// 32768 x 512 -> 64 11.7 (64: 16.9).
+// (256 rows and columns each).  Against always taking one of them, us: 64 x 4096 -> 4096 12.7 (64: 16.2, pairs: 27), 1024 x 4096 -> 512
+// 14.4 (64: 17), 4096 x 512 -> 512 8.6 (64: 10.3), 32768 x 512 -> 64 11.7 (64: 16.9).
 int64_t split_cost(int M, int N, int blocks, int SN)
 {
     const int64_t tiles = ceil_div(M, 128) * ceil_div(N, SN);
@@ -835,8 +840,8 @@ extern "C" hts_status hts_linear_gradient(const hts_linear_desc* d, const void* 
         bf16* dz = copy && (dx || dw) ? (bf16*)(ws + q.dz) : nullptr;
         float* part = dbias ? (float*)(ws + q.sums) : nullptr;
         const bool wide = N % 8 == 0 && as_is(dy, d->ld_dy) && (!pre || as_is(pre, d->ld_pre));
-        const int64_t blocks = ceil_div(M, kSumRows) * ceil_div(N, wide ? 256 : 32);
-        HTS_CUDA(launch_pdl(wide ? dz_kernel<8> : dz_kernel<1>, dim3((unsigned)blocks), dim3(32, 8), 0, s, (const bf16*)dy, d->ld_dy, (const bf16*)pre, d->ld_pre, M, N,
+        const int64_t blocks = ceil_div(M, kSumRows) * ceil_div(N, wide ? 128 : 32);
+        HTS_CUDA(launch_pdl(wide ? dz_kernel<4> : dz_kernel<1>, dim3((unsigned)blocks), dim3(32, 8), 0, s, (const bf16*)dy, d->ld_dy, (const bf16*)pre, d->ld_pre, M, N,
                             d->activation, dz, padded(N), act && dz_planes(M, N) > 1, part));
         note_launch();
         if (dz) g = Operand{dz, padded(N), act ? dz_planes(M, N) : 1};
