@@ -449,7 +449,7 @@ template <typename T, int LS> struct GradientShared {
 // channel) crosses LS lanes, what has to be added over channels (dB and dC, eight sums, two channels of which meet in the thread)
 // the others: in the first exchanges of each each lane keeps half of the sums and hands on the other half.  With eight states of one
 // channel in a thread, states and gradients in shared memory and the sums over channels read from there, shared memory
-// bounded it (105 accesses a warp and step): 1165 us for 128 x 256 steps of 1024 channels and 16 states, as long as this takes (1132),
+// bounded it (105 accesses a warp and step): 1165 us for 128 x 256 steps of 1024 channels and 16 states, as long as this took then (1132, with states in fours 1116),
 // which has 42 % of the accesses and is bound by latency: three warps a scheduler of 160 registers, 0.53 instructions a clock.  Four
 // with states of two steps (1201) or chunks of four (1077, but twice the memory for checks) do not change that much.
 template <typename T, int LS, bool WIDE>
